@@ -513,6 +513,224 @@ int tl_stream_read(const void* src, int64_t bytes, uint32_t* checksum, void* str
 int tl_gemm_noalloc(const void* A, const void* W, void* C, int64_t M, int64_t N, int64_t K,
                     const tl_layout_desc* layout, int32_t fetch_mode, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * A serving step around the projections: a paged key/value cache, attention
+ * over it, and the verification of drafted tokens.  Of a layer, tl_gemm makes
+ * the rows of queries, keys and values; tl_kv_append turns and stores them;
+ * tl_attn answers; tl_gemm takes its output on.  After the last layer and the
+ * head, tl_verify walks every sequence's drafted tokens, and tl_kv_keep moves
+ * the accepted ones' entries to where the sequence goes on.
+ * ------------------------------------------------------------------------- */
+
+/*
+ * A paged cache of one layer, owned by the caller.  Tokens live in slots:
+ * slot = page * page_tokens + place.  A page holds a block of page_tokens *
+ * head_dim elements per head in k, and one in v.  Elements are bf16
+ * (elem_bytes 2) or OCP E4M3 (elem_bytes 1) times 2^(x - 127), x one byte per
+ * token and head in k_exp and v_exp (NULL for bf16).  The order inside a block
+ * is the one in which the attention kernel's matrix operands load it, chunks
+ * of c = 16 / elem_bytes elements, t a token's place and d an element:
+ *   k      [page][head][t / 16][d / c][t % 16][d % c]
+ *   v      [page][head][t / 4c][d / 16][t % 16 / 4][d % 16][t % 4c / 16][t % 4]
+ *   k_exp  [page][head][t / 64][t % 16][t % 64 / 16]
+ *   v_exp  [page][head][t / 64][t % 16 / 4][t % 64 / 16][t % 4]
+ * All of it 16-byte aligned.  Nothing needs to be initialised: a slot is read
+ * only once a token was written to it.
+ */
+typedef struct tl_kv_cache {
+    void* k;
+    void* v;
+    uint8_t* k_exp;
+    uint8_t* v_exp;
+    int64_t num_pages;
+    int32_t page_tokens;   /* a power of two, 64 .. 4096 */
+    int32_t kv_heads;      /* 1 .. 1024 */
+    int32_t head_dim;      /* 64 or 128 */
+    int32_t elem_bytes;    /* 1 (E4M3) or 2 (bf16) */
+} tl_kv_cache;
+
+/* tl_kv_bytes -- host only: bytes of k (and of v) into *data, of k_exp (and
+ * v_exp; 0 for bf16) into *exps, for the cache's sizes (its pointers are not
+ * looked at).  Errors: TL_EINVAL for NULL pointers, num_pages < 1, more than
+ * 2^31 - 1 slots, or a page_tokens, kv_heads or elem_bytes outside the ranges
+ * above; TL_EUNSUPPORTED for another head_dim. */
+int tl_kv_bytes(const tl_kv_cache* cache, int64_t* data, int64_t* exps);
+
+/* Rotary positions.  Of every head's first rot_dim elements, pair i of
+ * rot_dim / 2 is turned by positions[axis][token] * inv_freq[i]: elements i and
+ * i + rot_dim / 2, or 2i and 2i + 1 (interleaved).  The pairs belong to the
+ * axes in order, sections[axis] of them each: one axis for text, or e.g. time,
+ * height and width for images and video. */
+typedef struct tl_rope {
+    const int32_t* positions;  /* device [axes][n] */
+    const float* inv_freq;     /* device [rot_dim / 2] */
+    int32_t rot_dim;           /* a multiple of 16, up to head_dim */
+    int32_t axes;              /* 1 .. 3 */
+    int32_t sections[3];       /* pairs of each axis: their sum is rot_dim / 2 */
+    int32_t interleaved;
+} tl_rope;
+
+enum { TL_IN_F32 = 0, TL_IN_BF16 = 1 };
+
+/*
+ * tl_kv_append -- the n rows of a QKV projection into the cache: queries and
+ * keys turned by rope (NULL: not), queries written as bf16, keys and values
+ * stored at slots[row].
+ *
+ * Q, K, V: device rows of q_heads (kv_heads) * head_dim elements, in_dtype
+ *          (TL_IN_F32 or TL_IN_BF16, tl_gemm's two outputs), ldq, ldk, ldv
+ *          elements apart: a whole projection's rows or columns of one.  Row
+ *          starts are 16-byte aligned.  Q may be NULL (then q_heads is 0 and
+ *          Q_out NULL), and so may K and V together (only queries then).
+ * slots:   device int32 [n]; one outside the cache stores nothing (padding
+ *          rows).  Two rows with one slot: one of them is stored, or a mix.
+ * Q_out:   device bf16 [n][q_heads][head_dim].
+ * Angles are reduced in 64 bits, everything else is computed in fp32 and
+ * rounded once, to nearest even.  E4M3: a token's head is stored with the
+ * smallest exponent e with max |x| <= 448 * 2^e, -126 <= e; scaling by 2^-e is
+ * exact (values below 2^-126 aside).  Infinities are stored as the largest
+ * value, NaNs as NaN (they do not count for the maximum).
+ * Errors: TL_EINVAL for a bad cache (see tl_kv_bytes), NULL or misaligned
+ * pointers (slots, positions, inv_freq 4-byte aligned), n < 0, negative
+ * q_heads, a row stride below a row's length or not a multiple of 16 bytes, a
+ * bad in_dtype or rope, outputs that overlap inputs or each other;
+ * TL_EUNSUPPORTED for q_heads above 4096, row strides above 2^30, or n rows
+ * whose heads need more than 2^31 - 1 workgroups.  n == 0 enqueues nothing.
+ */
+int tl_kv_append(const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv,
+                 int32_t in_dtype, int64_t n, int32_t q_heads, const int32_t* slots,
+                 const tl_rope* rope, void* Q_out, const tl_kv_cache* cache, void* stream);
+
+/*
+ * tl_kv_read -- entries back as values: K_out[i], V_out[i] = the entry at
+ * slots[i], bf16 [n][kv_heads][head_dim] (exact: a stored value has at most
+ * eight significant bits; E4M3 values times 2^-126 or less may round to
+ * subnormal bf16).  A slot outside the cache reads zeros.  Either output may
+ * be NULL.  Errors: TL_EINVAL for a bad cache, NULL or misaligned pointers,
+ * n < 0, both outputs NULL, or outputs that overlap the cache, slots or each
+ * other; TL_EUNSUPPORTED for more than 2^31 - 1 workgroups.  n == 0 enqueues
+ * nothing.
+ */
+int tl_kv_read(const tl_kv_cache* cache, const int32_t* slots, int64_t n, void* K_out, void* V_out, void* stream);
+
+/*
+ * tl_kv_keep -- after tl_verify: of every sequence s, the entries of the
+ * accepted nodes move to the front of the new tokens,
+ *     token starts[s] + i  <-  token starts[s] + path[s][i],  i < counts[s]
+ * as stored (no rounding).  Token t of a sequence is at page
+ * page_table[s][t / page_tokens], place t % page_tokens.
+ *
+ * page_table: device int32 [num_seqs][max_pages].
+ * starts:     device int32 [num_seqs], the first new token (the tree's root).
+ * path:       device int32 [num_seqs][max_path], as tl_verify writes it: node
+ *             i >= i of a rising list.  An entry with path[s][i] <= i moves
+ *             nothing; a token outside the table or the cache is neither read
+ *             nor written.
+ * counts:     device int32 [num_seqs], at most max_path used.
+ * Sequences must not share the pages that hold their new tokens.
+ * Errors: TL_EINVAL for a bad cache, NULL or misaligned pointers (4 bytes),
+ * num_seqs < 0, max_pages < 1, max_path < 1; TL_EUNSUPPORTED for max_path
+ * above 4096 or num_seqs * kv_heads above 2^31 - 1.  num_seqs == 0 enqueues
+ * nothing.
+ */
+int tl_kv_keep(const tl_kv_cache* cache, const int32_t* page_table, int64_t max_pages, const int32_t* starts,
+               const int32_t* path, int64_t max_path, const int32_t* counts, int32_t num_seqs, void* stream);
+
+/*
+ * tl_attn -- attention of the new tokens of every sequence over the cache,
+ * which holds them already (tl_kv_append first).  Sequence s has lens[s]
+ * tokens; the rows q_offsets[s] .. q_offsets[s + 1] - 1 of Q are its last n_s
+ * tokens.  For its new token i and query head h (key head h / (q_heads /
+ * kv_heads)), over the keys j that token i sees,
+ *     O[row][h] = sum_j softmax_j(scale * q . k_j) v_j
+ * Without a mask token i sees every token up to itself.  With one (a tree of
+ * drafted tokens) it sees the lens[s] - n_s tokens before the new ones, and of
+ * those new token b where bit b % 32 of mask[row][b / 32] is set; bits beyond
+ * mask_words * 32 count as clear.  A row that sees nothing gives zeros, and a
+ * key that a row does not see contributes nothing to it, whatever its entry
+ * holds (NaNs too).  One entry point serves single tokens, chains, trees and
+ * prompts.
+ *
+ * Q:          device bf16, rows of q_heads * head_dim elements, ldq apart.
+ * page_table: device int32 [num_seqs][max_pages]; a page outside the cache
+ *             holds keys that nobody sees.
+ * lens:       device int32 [num_seqs], clamped to [0, min(max_len, max_pages *
+ *             page_tokens)].
+ * q_offsets:  device int32 [num_seqs + 1], nondecreasing, from 0 to total_q,
+ *             clamped to that.
+ * mask:       device uint32 [total_q][mask_words], or NULL (causal).
+ * max_q, max_len: host bounds on n_s and lens[s]; with total_q they size the
+ *             launch (rows past a wrong bound are not computed).
+ * scale:      > 0 and finite.
+ * O:          device bf16 [total_q][q_heads][head_dim]; must not overlap the
+ *             inputs.
+ * Products run on MFMA with bf16 operands and fp32 sums: E4M3 keys times
+ * their scale and values are bf16 exactly, the probabilities (times the
+ * values' scale) are rounded to bf16; maxima, sums and the output are fp32
+ * until it is rounded.  Results are the same from call to call with the same
+ * bounds.  Keys of one sequence may be split over workgroups, whose partial
+ * results take library workspace of the stream (see "HIP graphs" above).
+ * Errors: TL_EINVAL for a bad cache, NULL or misaligned pointers (Q and O 16
+ * bytes, the rest 4), negative counts, max_pages < 1, q_heads not a positive
+ * multiple of kv_heads, a bad ldq (see tl_kv_append) or scale, mask_words < 1
+ * with a mask, or O overlapping an input; TL_EUNSUPPORTED for max_len or
+ * total_q * q_heads above 2^30, mask_words above 2^16, ldq above 2^30 or a
+ * grid above 2^31 - 1 workgroups; TL_ENOMEM if the workspace cannot be
+ * allocated.  total_q == 0 or num_seqs == 0 enqueues nothing.
+ */
+int tl_attn(const void* Q, int64_t ldq, const tl_kv_cache* cache, const int32_t* page_table, int64_t max_pages,
+            const int32_t* lens, const int32_t* q_offsets, const uint32_t* mask, int32_t mask_words,
+            int32_t num_seqs, int64_t total_q, int64_t max_q, int64_t max_len, int32_t q_heads, float scale,
+            void* O, void* stream);
+
+/*
+ * tl_verify -- drafted tokens against the target's probabilities.  The nodes of
+ * sequence s are rows node_offsets[s] .. node_offsets[s + 1] - 1; node 0 of
+ * them is the last token that is certain, every other node is a drafted token
+ * with an earlier node as its parent (a chain: parents[i] = i - 1).  With
+ * p_i = softmax(logits_i / temperature[s]) -- at temperature 0 (or below) all
+ * of it on the largest logit, the first of equal ones -- the walk starts at
+ * node 0 with the weights w = p_0 and their sum m = 1 and tries the node's
+ * children in order: child c with token x is accepted if
+ *     uniform[c] * q(x) * m < w(x)
+ * (q = the draft's distribution at the parent, draft[parent]; 1 without a
+ * draft: its tokens were certain).  Then the walk goes on from c.  Otherwise
+ *     w <- max(w / m - q, 0), m <- sum w;  without a draft w(x) <- 0, m <- m - w(x)
+ * and the next child is tried.  Where none is left, the next token is the
+ * largest w(v) / noise[s][v] (the first of equal ones): with noise drawn from
+ * the exponential distribution a sample of w, so that accepted and sampled
+ * tokens together follow the target.  If no w(v) > 0, p takes w's place.
+ *
+ * logits:       device [total_nodes][vocab] fp32 or bf16 (tl_out_dtype).
+ * node_offsets: device int32 [num_seqs + 1], nondecreasing, 0 to total_nodes.
+ * parents:      device int32 [total_nodes], local to the sequence (entry of
+ *               node 0 unused).  A child must come after its parent.
+ * tokens:       device int32 [total_nodes] (entry of node 0 unused); a child
+ *               with a token outside [0, vocab) is not tried.
+ * draft:        device [total_nodes][vocab] fp32 or bf16, or NULL.
+ * temperature:  device fp32 [num_seqs].
+ * uniform:      device fp32 [total_nodes] in [0, 1).
+ * noise:        device fp32 [num_seqs][vocab], > 0.
+ * max_nodes:    host bound on a sequence's nodes (further ones are ignored).
+ * path:         device int32 [num_seqs][max_nodes]: the accepted nodes from
+ *               node 0 on, local indexes, then -1.
+ * counts:       device int32 [num_seqs]: how many.
+ * next:         device int32 [num_seqs]: the token after them (0 if the
+ *               logits have no largest finite value; -1, and count 0, for a
+ *               sequence without nodes).
+ * Sums are fp32; nothing depends on the order of atomics.  Takes library
+ * workspace of the stream (see "HIP graphs" above).
+ * Errors: TL_EINVAL for NULL or misaligned pointers (logits, draft, noise 16
+ * bytes, the rest 4), vocab < 1, negative counts, max_nodes < 1 or a bad
+ * dtype; TL_EUNSUPPORTED for vocab or total_nodes above 2^26 or max_nodes
+ * above 4096; TL_ENOMEM as above.  num_seqs == 0 enqueues nothing.
+ */
+int tl_verify(const void* logits, int32_t logits_dtype, int64_t vocab, const int32_t* node_offsets,
+              const int32_t* parents, const int32_t* tokens, int32_t num_seqs, int64_t total_nodes,
+              int32_t max_nodes, const void* draft, int32_t draft_dtype, const float* temperature,
+              const float* uniform, const float* noise, int32_t* path, int32_t* counts, int32_t* next,
+              void* stream);
+
 /* tl_fetch_counter_read -- synchronises 'stream', stores the weight bytes
  * tallied by tl_gemm calls made on it with TL_FETCH_COUNT since the last read
  * into *bytes, and resets the tally (nothing else) to zero.  Errors: TL_EINVAL for NULL

@@ -13,14 +13,17 @@ the C names and argument order of ``include/tl.h``:
     tl_gemm_plan(M, N, K, layout, fetch_mode) -> dict
     tl_gemm_grouped / tl_gemm_grouped_swiglu (..., layout, fetch_mode, stream=None)
     tl_read_amp(M, N, K, tile_m, tile_n, tile_k, layout, G) -> dict
+    tl_kv_bytes / tl_kv_append / tl_kv_read / tl_kv_keep (a paged key/value cache)
+    tl_attn (attention over it), tl_verify (drafted tokens)
     tl_fetch_counter_read(stream=None) -> int
     tl_release()
     tl_strerror(status) -> str
 
 Pointer arguments accept a torch CUDA tensor or a raw integer address.
 ``layout`` is a :class:`LayoutDesc` (or a dict of its fields).  A few helpers
-(``repack``, ``gemm``, ``layout``) build outputs and descriptors for callers
-that just hold tensors.
+(``repack``, ``gemm``, ``layout``; ``kv_cache``, ``rope``, ``kv_append``,
+``kv_read``, ``kv_keep``, ``attention``, ``verify``) build outputs and
+descriptors for callers that just hold tensors.
 
 If libtl.so has not been built the first call raises ``ImportError``; there is
 no fallback path of any kind.
@@ -41,8 +44,10 @@ TL_FETCH_NATIVE, TL_FETCH_BLOCK, TL_FETCH_COUNT = 0, 1, 0x100
 
 EXPORTED = ("tl_tile_bytes", "tl_repack", "tl_unpack", "tl_gemm", "tl_gemm_noalloc", "tl_gemm_w8", "tl_gemm_plan", "tl_gemm_grouped", "tl_gemm_grouped_swiglu", "tl_read_amp",
             "tl_view_offsets", "tl_view_load", "tl_prefetch_degree", "tl_gemm_lgms", "tl_lgms_occupancy",
+            "tl_kv_bytes", "tl_kv_append", "tl_kv_read", "tl_kv_keep", "tl_attn", "tl_verify",
             "tl_stream_read", "tl_fetch_counter_read", "tl_release", "tl_strerror")
 TL_VIEW_MAX_RANK = 5
+TL_IN_F32, TL_IN_BF16 = 0, 1
 
 
 class View(ctypes.Structure):
@@ -94,6 +99,57 @@ class Plan(ctypes.Structure):
                 ("waves", ctypes.c_int32),
                 ("workgroups", ctypes.c_int64),
                 ("workspace_bytes", ctypes.c_int64)]
+
+
+class KVCacheDesc(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p),
+                ("k_exp", ctypes.c_void_p),
+                ("v_exp", ctypes.c_void_p),
+                ("num_pages", ctypes.c_int64),
+                ("page_tokens", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32),
+                ("elem_bytes", ctypes.c_int32)]
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = [("positions", ctypes.c_void_p),
+                ("inv_freq", ctypes.c_void_p),
+                ("rot_dim", ctypes.c_int32),
+                ("axes", ctypes.c_int32),
+                ("sections", ctypes.c_int32 * 3),
+                ("interleaved", ctypes.c_int32)]
+
+
+class KVCache:
+    """tl_kv_cache over tensors that it keeps alive: k and v [pages, kv_heads, page_tokens * head_dim] (uint8 holding
+    E4M3, or bfloat16), k_exp and v_exp uint8 [pages, kv_heads, page_tokens] (None for bfloat16)."""
+
+    def __init__(self, k, v, k_exp, v_exp, page_tokens, kv_heads, head_dim):
+        self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+        self.page_tokens, self.kv_heads, self.head_dim = page_tokens, kv_heads, head_dim
+        self.elem_bytes = k.element_size()
+        block = page_tokens * kv_heads * head_dim
+        self.num_pages = k.numel() // block
+        if k.numel() != self.num_pages * block or v.numel() != k.numel() or v.element_size() != k.element_size():
+            raise ValueError("k and v must hold whole pages of the same type")
+        if (k_exp is None) != (self.elem_bytes == 2) or (v_exp is None) != (self.elem_bytes == 2):
+            raise ValueError("8-bit caches have exponents, and only they")
+        for x in (k_exp, v_exp):
+            if x is not None and (x.element_size() != 1 or x.numel() != self.num_pages * page_tokens * kv_heads):
+                raise ValueError("one exponent byte per token and head")
+        self.desc = KVCacheDesc(_ptr(k), _ptr(v), _ptr(k_exp), _ptr(v_exp), self.num_pages, page_tokens, kv_heads,
+                                head_dim, self.elem_bytes)
+
+
+class Rope:
+    """tl_rope over tensors that it keeps alive."""
+
+    def __init__(self, positions, inv_freq, sections, interleaved, rot_dim):
+        self.positions, self.inv_freq = positions, inv_freq
+        self.desc = RopeDesc(_ptr(positions), _ptr(inv_freq), rot_dim, len(sections),
+                             (ctypes.c_int32 * 3)(*(list(sections) + [0] * (3 - len(sections)))), int(interleaved))
 
 
 def _struct_dict(s):
@@ -153,6 +209,19 @@ def load_library():
     lib.tl_read_amp.restype = ctypes.c_int
     lib.tl_read_amp.argtypes = [i64, i64, i64, i32, i32, i32, ctypes.POINTER(LayoutDesc), i64,
                                 ctypes.POINTER(Amp)]
+    f32, cache = ctypes.c_float, ctypes.POINTER(KVCacheDesc)
+    lib.tl_kv_bytes.restype = ctypes.c_int
+    lib.tl_kv_bytes.argtypes = [cache, ctypes.POINTER(i64), ctypes.POINTER(i64)]
+    lib.tl_kv_append.restype = ctypes.c_int
+    lib.tl_kv_append.argtypes = [p, i64, p, i64, p, i64, i32, i64, i32, p, ctypes.POINTER(RopeDesc), p, cache, p]
+    lib.tl_kv_read.restype = ctypes.c_int
+    lib.tl_kv_read.argtypes = [cache, p, i64, p, p, p]
+    lib.tl_kv_keep.restype = ctypes.c_int
+    lib.tl_kv_keep.argtypes = [cache, p, i64, p, p, i64, p, i32, p]
+    lib.tl_attn.restype = ctypes.c_int
+    lib.tl_attn.argtypes = [p, i64, cache, p, i64, p, p, p, i32, i32, i64, i64, i64, i32, f32, p, p]
+    lib.tl_verify.restype = ctypes.c_int
+    lib.tl_verify.argtypes = [p, i32, i64, p, p, p, i32, i64, i32, p, i32, p, p, p, p, p, p, p]
     lib.tl_stream_read.restype = ctypes.c_int
     lib.tl_stream_read.argtypes = [p, i64, p, p]
     lib.tl_fetch_counter_read.restype = ctypes.c_int
@@ -315,6 +384,51 @@ def tl_read_amp(M, N, K, tile_m, tile_n, tile_k, layout, G) -> dict:
     return _struct_dict(out)
 
 
+def _cache_ref(cache):
+    return ctypes.byref(cache.desc if isinstance(cache, KVCache) else cache)
+
+
+def tl_kv_bytes(cache) -> tuple[int, int]:
+    """(bytes of k and of v, bytes of k_exp and of v_exp) for a KVCacheDesc's sizes."""
+    data, exps = ctypes.c_int64(0), ctypes.c_int64(0)
+    _check(load_library().tl_kv_bytes(_cache_ref(cache), ctypes.byref(data), ctypes.byref(exps)), "tl_kv_bytes")
+    return data.value, exps.value
+
+
+def tl_kv_append(Q, ldq, K, ldk, V, ldv, in_dtype, n, q_heads, slots, rope, Q_out, cache, stream=None):
+    """rope: a Rope or None; Q, K, V: raw addresses where rows are not contiguous."""
+    r = None if rope is None else ctypes.byref(rope.desc if isinstance(rope, Rope) else rope)
+    _check(load_library().tl_kv_append(_ptr(Q), ldq, _ptr(K), ldk, _ptr(V), ldv, in_dtype, n, q_heads, _ptr(slots), r,
+                                       _ptr(Q_out), _cache_ref(cache), _stream(stream)), "tl_kv_append")
+
+
+def tl_kv_read(cache, slots, n, K_out, V_out, stream=None):
+    _check(load_library().tl_kv_read(_cache_ref(cache), _ptr(slots), n, _ptr(K_out), _ptr(V_out), _stream(stream)),
+           "tl_kv_read")
+
+
+def tl_kv_keep(cache, page_table, max_pages, starts, path, max_path, counts, num_seqs, stream=None):
+    _check(load_library().tl_kv_keep(_cache_ref(cache), _ptr(page_table), max_pages, _ptr(starts), _ptr(path), max_path,
+                                     _ptr(counts), num_seqs, _stream(stream)), "tl_kv_keep")
+
+
+def tl_attn(Q, ldq, cache, page_table, max_pages, lens, q_offsets, mask, mask_words, num_seqs, total_q, max_q, max_len,
+            q_heads, scale, O, stream=None):
+    """mask may be None (causal)."""
+    _check(load_library().tl_attn(_ptr(Q), ldq, _cache_ref(cache), _ptr(page_table), max_pages, _ptr(lens),
+                                  _ptr(q_offsets), _ptr(mask), mask_words, num_seqs, total_q, max_q, max_len, q_heads,
+                                  scale, _ptr(O), _stream(stream)), "tl_attn")
+
+
+def tl_verify(logits, logits_dtype, vocab, node_offsets, parents, tokens, num_seqs, total_nodes, max_nodes, draft,
+              draft_dtype, temperature, uniform, noise, path, counts, next_token, stream=None):
+    """draft may be None (drafted tokens were certain)."""
+    _check(load_library().tl_verify(_ptr(logits), logits_dtype, vocab, _ptr(node_offsets), _ptr(parents), _ptr(tokens),
+                                    num_seqs, total_nodes, max_nodes, _ptr(draft), draft_dtype, _ptr(temperature),
+                                    _ptr(uniform), _ptr(noise), _ptr(path), _ptr(counts), _ptr(next_token),
+                                    _stream(stream)), "tl_verify")
+
+
 def tl_stream_read(src, nbytes, checksum, stream=None):
     """checksum: a device uint32/int32 tensor of one element; the XOR of src's 32-bit words is XORed into it."""
     _check(load_library().tl_stream_read(_ptr(src), nbytes, _ptr(checksum), _stream(stream)), "tl_stream_read")
@@ -382,3 +496,145 @@ def gemm(A, W, N, desc: LayoutDesc, fetch_mode=TL_FETCH_BLOCK, out=None, stream=
     C = torch.empty((M, N), dtype=dt, device=A.device) if out is None else out
     tl_gemm(A, W, C, M, N, K, desc, fetch_mode, stream)
     return C
+
+
+def kv_cache(num_pages, kv_heads, head_dim, page_tokens=64, elem_bytes=1, device="cuda") -> KVCache:
+    """An empty cache: 8-bit (E4M3 with scales) or, with elem_bytes=2, bf16."""
+    import torch
+    dt = torch.uint8 if elem_bytes == 1 else torch.bfloat16
+    data, exps = tl_kv_bytes(KVCacheDesc(None, None, None, None, num_pages, page_tokens, kv_heads, head_dim, elem_bytes))
+    k, v = (torch.empty((num_pages, kv_heads, page_tokens * head_dim), dtype=dt, device=device) for _ in range(2))
+    assert k.numel() * k.element_size() == data
+    ke, ve = (torch.empty((num_pages, kv_heads, page_tokens), dtype=torch.uint8, device=device) if exps else None
+              for _ in range(2))
+    return KVCache(k, v, ke, ve, page_tokens, kv_heads, head_dim)
+
+
+def rope(positions, inv_freq, sections=None, interleaved=False) -> Rope:
+    """Rotary positions: int32 [axes, n] (or [n]) and float32 [rot_dim / 2]; sections: pairs of each axis (one axis: all)."""
+    import torch
+    if positions.dtype != torch.int32 or inv_freq.dtype != torch.float32:
+        raise ValueError("positions are int32 and inv_freq float32")
+    pairs = inv_freq.numel()
+    sections = (pairs,) if sections is None else tuple(int(x) for x in sections)
+    if positions.numel() and positions.numel() % len(sections):
+        raise ValueError("positions need one row per axis")
+    return Rope(positions, inv_freq, sections, interleaved, 2 * pairs)
+
+
+def _rows(x, heads, head_dim):
+    """(address, elements between rows) of [n, heads * head_dim] or [n, heads, head_dim] rows, each without gaps."""
+    if not x.is_cuda:
+        raise ValueError("libtl needs device tensors")
+    tail = x.shape[1:]
+    if x.dim() not in (2, 3) or tail.numel() != heads * head_dim or x.stride(-1) != 1 or \
+            (x.dim() == 3 and x.shape[1] > 1 and x.stride(1) != x.shape[2]):
+        raise ValueError(f"rows of {heads} x {head_dim} elements without gaps are needed, not {tuple(x.shape)}")
+    return x.data_ptr(), x.stride(0) if x.shape[0] > 1 else heads * head_dim
+
+
+def _int32(*tensors):
+    import torch
+    for x in tensors:
+        if x is not None and x.dtype not in (torch.int32, torch.uint32):
+            raise ValueError("indexes, offsets and masks are int32")
+
+
+def _in_dtype(x):
+    import torch
+    if x.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("float32 or bfloat16 is needed")
+    return TL_IN_BF16 if x.dtype == torch.bfloat16 else TL_IN_F32
+
+
+def kv_append(q, k, v, cache: KVCache, slots, rope=None, q_out=None, stream=None):
+    """Rows of a QKV projection (tensors, or column ranges of one) into the cache at slots; returns the queries, turned by
+    rope, as bf16 [n, q_heads, head_dim].  q may be None, and so may k and v."""
+    import torch
+    some = q if q is not None else k
+    n, D, H = some.shape[0], cache.head_dim, cache.kv_heads
+    heads = 0 if q is None else q.shape[1:].numel() // D
+    _int32(slots)
+    for x in (q, k, v):
+        if x is not None and (x.dtype != some.dtype or x.shape[0] != n):
+            raise ValueError("queries, keys and values are rows of one type")
+    if k is not None and slots.numel() != n:
+        raise ValueError("one slot per row")
+    if rope is not None and rope.positions.numel() != n * rope.desc.axes:
+        raise ValueError("one position per axis and row")
+    (qp, ldq), (kp, ldk), (vp, ldv) = ((None, 0) if x is None else _rows(x, h, D) for x, h in ((q, heads), (k, H), (v, H)))
+    if q is not None and q_out is None:
+        q_out = torch.empty((n, heads, D), dtype=torch.bfloat16, device=q.device)
+    if q is not None and (q_out.dtype != torch.bfloat16 or q_out.numel() != n * heads * D):
+        raise ValueError("q_out is bfloat16 [n, q_heads, head_dim]")
+    tl_kv_append(qp, ldq, kp, ldk, vp, ldv, _in_dtype(some), n, heads, slots, rope, q_out, cache, stream)
+    return q_out
+
+
+def kv_read(cache: KVCache, slots, k_out=None, v_out=None, stream=None):
+    """bf16 keys and values [n, kv_heads, head_dim] of the given slots."""
+    import torch
+    _int32(slots)
+    n = slots.numel()
+    shape = (n, cache.kv_heads, cache.head_dim)
+    k_out = torch.empty(shape, dtype=torch.bfloat16, device=slots.device) if k_out is None else k_out
+    v_out = torch.empty(shape, dtype=torch.bfloat16, device=slots.device) if v_out is None else v_out
+    for x in (k_out, v_out):
+        if x.dtype != torch.bfloat16 or x.numel() != n * cache.kv_heads * cache.head_dim:
+            raise ValueError("outputs are bfloat16 [n, kv_heads, head_dim]")
+    tl_kv_read(cache, slots, n, k_out, v_out, stream)
+    return k_out, v_out
+
+
+def kv_keep(cache: KVCache, page_table, starts, path, counts, stream=None):
+    """Moves the entries of every sequence's accepted path (as verify returns it) to the front of its new tokens."""
+    _int32(page_table, starts, path, counts)
+    B = page_table.shape[0]
+    if starts.numel() != B or counts.numel() != B or path.shape[0] != B:
+        raise ValueError("one row per sequence")
+    tl_kv_keep(cache, page_table, page_table.shape[1], starts, path, path.shape[1], counts, B, stream)
+
+
+def attention(q, cache: KVCache, page_table, lens, q_offsets, max_q, max_len, scale, mask=None, out=None, stream=None):
+    """Attention of the new tokens q [total_q, q_heads, head_dim] (bf16) over the cache: bf16 of q's shape.  mask: int32
+    [total_q, words] of the new tokens that each new token sees, or None (causal)."""
+    import torch
+    if q.dtype != torch.bfloat16:
+        raise ValueError("queries are bfloat16")
+    _int32(page_table, lens, q_offsets, mask)
+    total, B, D = q.shape[0], lens.numel(), cache.head_dim
+    heads = q.shape[1:].numel() // D
+    if page_table.shape[0] != B or q_offsets.numel() != B + 1 or (mask is not None and mask.shape[0] != total):
+        raise ValueError("one row per sequence, one more offset, one mask row per query row")
+    qp, ldq = _rows(q, heads, D)
+    if out is None:
+        out = torch.empty((total, heads, D), dtype=torch.bfloat16, device=q.device)
+    if out.dtype != torch.bfloat16 or out.numel() != total * heads * D:
+        raise ValueError("out is bfloat16 [total_q, q_heads, head_dim]")
+    tl_attn(qp, ldq, cache, page_table, page_table.shape[1], lens, q_offsets, mask, 0 if mask is None else mask.shape[1],
+            B, total, max_q, max_len, heads, scale, out, stream)
+    return out
+
+
+def verify(logits, node_offsets, parents, tokens, temperature, uniform, noise, max_nodes, draft=None, out=None,
+           stream=None):
+    """(path int32 [sequences, max_nodes], counts, next): the drafted tokens that stay, and the token after them."""
+    import torch
+    _int32(node_offsets, parents, tokens)
+    total, vocab = logits.shape
+    B = temperature.numel()
+    if any(x.dtype != torch.float32 for x in (temperature, uniform, noise)):
+        raise ValueError("temperature, uniform and noise are float32")
+    if node_offsets.numel() != B + 1 or any(x.numel() != total for x in (parents, tokens, uniform)) or \
+            noise.numel() != B * vocab or (draft is not None and draft.shape != logits.shape):
+        raise ValueError("sizes of logits, nodes and sequences do not agree")
+    if out is None:
+        out = (torch.empty((B, max_nodes), dtype=torch.int32, device=logits.device),
+               torch.empty(B, dtype=torch.int32, device=logits.device),
+               torch.empty(B, dtype=torch.int32, device=logits.device))
+    _int32(*out)
+    if [x.numel() for x in out] != [B * max_nodes, B, B]:
+        raise ValueError("out is (path, counts, next)")
+    tl_verify(logits, _in_dtype(logits), vocab, node_offsets, parents, tokens, B, total, max_nodes, draft,
+              TL_IN_F32 if draft is None else _in_dtype(draft), temperature, uniform, noise, *out, stream)
+    return out

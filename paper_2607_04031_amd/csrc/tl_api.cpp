@@ -875,6 +875,16 @@ bool medium_grouped(const Plan& p, const tl_layout_desc* d, int64_t num_groups, 
 }
 
 }  // namespace
+
+int stream_workspace(hipStream_t stream, size_t bytes, std::shared_ptr<void>* keep, void** ws) {
+    StateRef st;
+    const int rc = get_state(stream, bytes, &st);
+    if (rc != TL_OK) return rc;
+    *keep = st.keep;
+    *ws = st.ws;
+    return TL_OK;
+}
+
 }  // namespace tl
 
 using namespace tl;

@@ -3,6 +3,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <memory>
 
 #include <hip/hip_runtime.h>
 
@@ -208,6 +209,11 @@ __host__ __device__ inline int64_t view_offset(const ViewProgram& P, int64_t e) 
     }
     return off;
 }
+
+// At least 'bytes' of the stream's library workspace (grown by replacement),
+// alive as long as *keep; what it holds is the call's until the next call on
+// the stream.
+int stream_workspace(hipStream_t stream, size_t bytes, std::shared_ptr<void>* keep, void** ws);
 
 // reads bytes (a multiple of 16) of src once and XORs its 32-bit words
 // into *checksum (one kernel; nothing for bytes = 0)

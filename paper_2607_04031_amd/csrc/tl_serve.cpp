@@ -1,0 +1,273 @@
+// C ABI of the serving-step operators: argument validation, the attention
+// plan, dispatch.  Nothing is enqueued unless every check passes.
+#include <algorithm>
+#include <cmath>
+#include <memory>
+
+#include "tl_internal.h"
+#include "tl_serve.h"
+
+namespace tl {
+namespace {
+
+constexpr int64_t kMaxGrid = 0x7fffffff;
+constexpr int64_t kMaxStride = int64_t(1) << 30;
+constexpr int kMaxNodes = 4096;
+
+bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+bool bad_pointer(const void* p, uintptr_t to) { return !p || !aligned(p, to); }
+
+struct Range {
+    const void* p;
+    int64_t bytes;
+};
+bool overlap(const Range& a, const Range& b) {
+    if (!a.p || !b.p || a.bytes <= 0 || b.bytes <= 0) return false;
+    const auto x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+    return x < y + uintptr_t(b.bytes) && y < x + uintptr_t(a.bytes);
+}
+
+// The cache's sizes; data and exps: bytes of k (v) and of k_exp (v_exp).
+int check_sizes(const tl_kv_cache* c, int64_t* data, int64_t* exps) {
+    if (!c || c->num_pages < 1 || !is_pow2(c->page_tokens) || c->page_tokens < 64 || c->page_tokens > 4096) return TL_EINVAL;
+    if (c->kv_heads < 1 || c->kv_heads > 1024 || (c->elem_bytes != 1 && c->elem_bytes != 2)) return TL_EINVAL;
+    if (c->num_pages > kMaxGrid / c->page_tokens) return TL_EINVAL;
+    if (c->head_dim != 64 && c->head_dim != 128) return TL_EUNSUPPORTED;
+    const int64_t tokens = c->num_pages * c->page_tokens * c->kv_heads;
+    *data = tokens * c->head_dim * c->elem_bytes;
+    *exps = c->elem_bytes == 1 ? tokens : 0;
+    return TL_OK;
+}
+
+int check_cache(const tl_kv_cache* c, int64_t* data, int64_t* exps, KvView* view) {
+    const int rc = check_sizes(c, data, exps);
+    if (rc != TL_OK) return rc;
+    if (bad_pointer(c->k, 16) || bad_pointer(c->v, 16)) return TL_EINVAL;
+    if (c->elem_bytes == 1 && (bad_pointer(c->k_exp, 16) || bad_pointer(c->v_exp, 16))) return TL_EINVAL;
+    *view = KvView{static_cast<uint8_t*>(c->k), static_cast<uint8_t*>(c->v), c->k_exp, c->v_exp, c->num_pages,
+                   ilog2(c->page_tokens), c->kv_heads};
+    return TL_OK;
+}
+
+bool hits_cache(const tl_kv_cache* c, int64_t data, int64_t exps, const Range& r) {
+    return overlap(r, {c->k, data}) || overlap(r, {c->v, data}) || overlap(r, {c->k_exp, exps}) || overlap(r, {c->v_exp, exps});
+}
+
+int done(hipError_t e) { return e == hipSuccess ? TL_OK : TL_EHIP; }
+
+// Bytes from the first row's start to the last row's end.
+int64_t span(int64_t rows, int64_t ld, int64_t width, int64_t elem) { return rows > 0 ? ((rows - 1) * ld + width) * elem : 0; }
+
+}  // namespace
+
+// Rows per workgroup: the fewest of 16, 32 and 64 that hold a sequence's rows
+// of one key head.  Units of keys: as many as give about kTargetWorkgroups
+// workgroups, each at least one chunk per wave long.
+int64_t plan_attn(AttnLaunch* a, int head_dim, int) {
+    constexpr int64_t kTargetWorkgroups = 2048;
+    const int64_t group = a->q_heads / a->c.heads, most = a->max_q * group;
+    a->rows = most <= 16 ? 16 : most <= 32 ? 32 : 64;
+    a->max_tiles = std::min(a->num_seqs * ((most + a->rows - 1) / a->rows), a->total_q * group / a->rows + a->num_seqs);
+    const int64_t chunks = std::max<int64_t>(1, (a->max_len + 63) / 64), tiles = a->max_tiles * a->c.heads;
+    const int64_t units = std::max<int64_t>(1, std::min((chunks + 3) / 4, (kTargetWorkgroups + tiles - 1) / tiles));
+    a->chunks_per_unit = int(((chunks + units - 1) / units + 3) / 4 * 4);
+    a->max_units = int((chunks + a->chunks_per_unit - 1) / a->chunks_per_unit);
+    return a->max_units > 1 ? tiles * a->max_units * a->rows * (head_dim + 2) : 0;
+}
+
+}  // namespace tl
+
+using namespace tl;
+
+extern "C" {
+
+int tl_kv_bytes(const tl_kv_cache* cache, int64_t* data, int64_t* exps) {
+    if (!data || !exps) return TL_EINVAL;
+    int64_t d, e;
+    const int rc = check_sizes(cache, &d, &e);
+    if (rc != TL_OK) return rc;
+    *data = d;
+    *exps = e;
+    return TL_OK;
+}
+
+int tl_kv_append(const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv, int32_t in_dtype,
+                 int64_t n, int32_t q_heads, const int32_t* slots, const tl_rope* rope, void* Q_out,
+                 const tl_kv_cache* cache, void* stream) {
+    int64_t data, exps;
+    KvAppendLaunch a{};
+    const int rc = check_cache(cache, &data, &exps, &a.c);
+    if (rc != TL_OK) return rc;
+    if (n < 0 || q_heads < 0 || (in_dtype != TL_IN_F32 && in_dtype != TL_IN_BF16)) return TL_EINVAL;
+    if (n == 0) return TL_OK;
+    if ((K == nullptr) != (V == nullptr) || (Q == nullptr) != (q_heads == 0) || (Q == nullptr) != (Q_out == nullptr)) return TL_EINVAL;
+    if (!Q && !K) return TL_EINVAL;
+    if (q_heads > 4096) return TL_EUNSUPPORTED;
+    const int D = cache->head_dim, in = in_dtype == TL_IN_F32 ? 4 : 2;
+    const void* src[3] = {Q, K, V};
+    const int64_t ld[3] = {ldq, ldk, ldv};
+    const int heads[3] = {q_heads, K ? cache->kv_heads : 0, K ? cache->kv_heads : 0};
+    for (int i = 0; i < 3; ++i) {
+        a.src[i] = src[i];
+        a.ld[i] = ld[i];
+        a.heads[i] = heads[i];
+        if (!src[i]) continue;
+        if (!aligned(src[i], 16) || ld[i] < int64_t(heads[i]) * D || ld[i] * in % 16) return TL_EINVAL;
+        if (ld[i] > kMaxStride) return TL_EUNSUPPORTED;
+    }
+    if (K && bad_pointer(slots, 4)) return TL_EINVAL;
+    if (Q && !aligned(Q_out, 16)) return TL_EINVAL;
+    a.slots = K ? slots : nullptr;
+    if (rope) {
+        if (rope->axes < 1 || rope->axes > 3 || rope->rot_dim < 16 || rope->rot_dim > D || rope->rot_dim % 16) return TL_EINVAL;
+        if (bad_pointer(rope->positions, 4) || bad_pointer(rope->inv_freq, 4)) return TL_EINVAL;
+        int64_t pairs = 0;
+        for (int i = 0; i < rope->axes; ++i) {
+            if (rope->sections[i] < 0) return TL_EINVAL;
+            a.sections[i] = rope->sections[i];
+            pairs += rope->sections[i];
+        }
+        if (pairs != rope->rot_dim / 2) return TL_EINVAL;
+        a.positions = rope->positions;
+        a.inv_freq = rope->inv_freq;
+        a.rot_dim = rope->rot_dim;
+        a.interleaved = rope->interleaved != 0;
+    }
+    const int64_t all = int64_t(heads[0]) + heads[1] + heads[2];
+    if (n > kMaxGrid / all) return TL_EUNSUPPORTED;
+    const Range out = {Q_out, n * q_heads * D * 2};
+    for (int i = 0; i < 3; ++i) {
+        const Range r = {src[i], span(n, ld[i], int64_t(heads[i]) * D, in)};
+        if (overlap(out, r) || (K && hits_cache(cache, data, exps, r))) return TL_EINVAL;
+    }
+    if (K && hits_cache(cache, data, exps, out)) return TL_EINVAL;
+    a.src_f32 = in_dtype == TL_IN_F32;
+    a.n = n;
+    a.q_out = static_cast<uint16_t*>(Q_out);
+    return done(launch_kv_append(a, D, cache->elem_bytes, (hipStream_t)stream));
+}
+
+int tl_kv_read(const tl_kv_cache* cache, const int32_t* slots, int64_t n, void* K_out, void* V_out, void* stream) {
+    int64_t data, exps;
+    KvView view;
+    const int rc = check_cache(cache, &data, &exps, &view);
+    if (rc != TL_OK) return rc;
+    if (n < 0) return TL_EINVAL;
+    if (n == 0) return TL_OK;
+    if (bad_pointer(slots, 4) || (!K_out && !V_out) || !aligned(K_out, 16) || !aligned(V_out, 16)) return TL_EINVAL;
+    const int64_t row = int64_t(cache->kv_heads) * cache->head_dim;
+    if (n > kMaxGrid / (row / 8) * 256) return TL_EUNSUPPORTED;
+    const Range k = {K_out, n * row * 2}, v = {V_out, n * row * 2}, s = {slots, n * 4};
+    if (overlap(k, v) || overlap(k, s) || overlap(v, s)) return TL_EINVAL;
+    if (hits_cache(cache, data, exps, k) || hits_cache(cache, data, exps, v)) return TL_EINVAL;
+    return done(launch_kv_read(view, cache->head_dim, cache->elem_bytes, slots, n, static_cast<uint16_t*>(K_out),
+                               static_cast<uint16_t*>(V_out), (hipStream_t)stream));
+}
+
+int tl_kv_keep(const tl_kv_cache* cache, const int32_t* page_table, int64_t max_pages, const int32_t* starts,
+               const int32_t* path, int64_t max_path, const int32_t* counts, int32_t num_seqs, void* stream) {
+    int64_t data, exps;
+    KvKeepLaunch a{};
+    const int rc = check_cache(cache, &data, &exps, &a.c);
+    if (rc != TL_OK) return rc;
+    if (num_seqs < 0 || max_pages < 1 || max_path < 1) return TL_EINVAL;
+    if (num_seqs == 0) return TL_OK;
+    if (bad_pointer(page_table, 4) || bad_pointer(starts, 4) || bad_pointer(path, 4) || bad_pointer(counts, 4)) return TL_EINVAL;
+    if (max_path > kMaxNodes || num_seqs > kMaxGrid / cache->kv_heads) return TL_EUNSUPPORTED;
+    a.page_table = page_table;
+    a.max_pages = max_pages;
+    a.starts = starts;
+    a.path = path;
+    a.counts = counts;
+    a.num_seqs = num_seqs;
+    a.max_path = int(max_path);
+    return done(launch_kv_keep(a, cache->head_dim, cache->elem_bytes, (hipStream_t)stream));
+}
+
+int tl_attn(const void* Q, int64_t ldq, const tl_kv_cache* cache, const int32_t* page_table, int64_t max_pages,
+            const int32_t* lens, const int32_t* q_offsets, const uint32_t* mask, int32_t mask_words, int32_t num_seqs,
+            int64_t total_q, int64_t max_q, int64_t max_len, int32_t q_heads, float scale, void* O, void* stream) {
+    int64_t data, exps;
+    AttnLaunch a{};
+    const int rc = check_cache(cache, &data, &exps, &a.c);
+    if (rc != TL_OK) return rc;
+    if (num_seqs < 0 || total_q < 0 || max_q < 0 || max_len < 0 || max_pages < 1) return TL_EINVAL;
+    if (q_heads < 1 || q_heads % cache->kv_heads || !(scale > 0.f) || !std::isfinite(scale)) return TL_EINVAL;
+    if (mask && (mask_words < 1 || !aligned(mask, 4))) return TL_EINVAL;
+    const int D = cache->head_dim;
+    const int64_t width = int64_t(q_heads) * D;
+    if (total_q > 0 && num_seqs > 0) {
+        if (bad_pointer(Q, 16) || bad_pointer(O, 16) || bad_pointer(page_table, 4) || bad_pointer(lens, 4) || bad_pointer(q_offsets, 4)) return TL_EINVAL;
+        if (ldq < width || ldq % 8) return TL_EINVAL;
+    }
+    if (ldq > kMaxStride || max_len > kMaxStride || q_heads > kMaxStride / std::max<int64_t>(total_q, 1) || (mask && mask_words > 65536)) return TL_EUNSUPPORTED;
+    if (total_q == 0 || num_seqs == 0 || max_q == 0) return TL_OK;
+    if (max_pages > kMaxGrid) return TL_EUNSUPPORTED;
+    const Range out = {O, total_q * width * 2};
+    if (overlap(out, {Q, span(total_q, ldq, width, 2)}) || hits_cache(cache, data, exps, out) ||
+        overlap(out, {mask, total_q * mask_words * 4}) || overlap(out, {page_table, num_seqs * max_pages * 4}) ||
+        overlap(out, {lens, int64_t(num_seqs) * 4}) || overlap(out, {q_offsets, (int64_t(num_seqs) + 1) * 4})) return TL_EINVAL;
+    a.q = static_cast<const uint16_t*>(Q);
+    a.ldq = ldq;
+    a.page_table = page_table;
+    a.max_pages = max_pages;
+    a.lens = lens;
+    a.q_offsets = q_offsets;
+    a.mask = mask;
+    a.mask_words = mask_words;
+    a.num_seqs = num_seqs;
+    a.total_q = total_q;
+    a.max_q = std::min(max_q, total_q);
+    a.max_len = max_len;
+    a.q_heads = q_heads;
+    a.scale_log2 = scale * 1.44269504088896340736f;
+    a.out = static_cast<uint16_t*>(O);
+    const int64_t floats = plan_attn(&a, D, cache->elem_bytes);
+    if (a.max_tiles * a.c.heads > kMaxGrid / a.max_units) return TL_EUNSUPPORTED;
+    std::shared_ptr<void> keep;
+    if (floats > 0) {
+        void* ws = nullptr;
+        const int st = stream_workspace((hipStream_t)stream, size_t(floats) * 4, &keep, &ws);
+        if (st != TL_OK) return st;
+        a.ws = static_cast<float*>(ws);
+    }
+    return done(launch_attn(a, D, cache->elem_bytes, (hipStream_t)stream));
+}
+
+int tl_verify(const void* logits, int32_t logits_dtype, int64_t vocab, const int32_t* node_offsets, const int32_t* parents,
+              const int32_t* tokens, int32_t num_seqs, int64_t total_nodes, int32_t max_nodes, const void* draft,
+              int32_t draft_dtype, const float* temperature, const float* uniform, const float* noise, int32_t* path,
+              int32_t* counts, int32_t* next, void* stream) {
+    if (vocab < 1 || num_seqs < 0 || total_nodes < 0 || max_nodes < 1) return TL_EINVAL;
+    if (logits_dtype != TL_OUT_F32 && logits_dtype != TL_OUT_BF16) return TL_EINVAL;
+    if (draft && draft_dtype != TL_OUT_F32 && draft_dtype != TL_OUT_BF16) return TL_EINVAL;
+    if (num_seqs == 0) return TL_OK;
+    if (bad_pointer(node_offsets, 4) || bad_pointer(temperature, 4) || bad_pointer(path, 4) || bad_pointer(counts, 4) || bad_pointer(next, 4)) return TL_EINVAL;
+    if (bad_pointer(noise, 16) || !aligned(draft, 16)) return TL_EINVAL;
+    if (total_nodes > 0 && (bad_pointer(logits, 16) || bad_pointer(parents, 4) || bad_pointer(tokens, 4) || bad_pointer(uniform, 4))) return TL_EINVAL;
+    if (vocab > (1 << 26) || total_nodes > (1 << 26) || max_nodes > kMaxNodes || num_seqs > (1 << 24)) return TL_EUNSUPPORTED;
+    VerifyLaunch a{};
+    a.logits = logits;
+    a.logits_bf16 = logits_dtype == TL_OUT_BF16;
+    a.vocab = vocab;
+    a.offsets = node_offsets;
+    a.parents = parents;
+    a.tokens = tokens;
+    a.num_seqs = num_seqs;
+    a.total = total_nodes;
+    a.max_nodes = max_nodes;
+    a.draft = draft;
+    a.draft_bf16 = draft && draft_dtype == TL_OUT_BF16;
+    a.temperature = temperature;
+    a.uniform = uniform;
+    a.noise = noise;
+    a.path = path;
+    a.counts = counts;
+    a.next = next;
+    std::shared_ptr<void> keep;
+    const int st = stream_workspace((hipStream_t)stream, size_t(verify_workspace_bytes(vocab, total_nodes, num_seqs, max_nodes)), &keep, &a.ws);
+    if (st != TL_OK) return st;
+    return done(launch_verify(a, (hipStream_t)stream));
+}
+
+}  // extern "C"
