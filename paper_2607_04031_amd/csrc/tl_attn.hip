@@ -16,390 +16,439 @@
 // values' scale being rounded to bf16 in any case.
 #include <hip/hip_runtime.h>
 
-#include "tl_serve.h"
-#include "tl_serve_device.h"
+#include <type_traits>
+
+#include "tl_attn_device.h"
 
 namespace tl {
 namespace {
 
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
+constexpr float kSlack = 8.f;
 
-// Sequence of a flat tile index and the tile's place in it: tiles go sequence
-// by sequence.  Every lane of every wave calls it; false past the last tile.
-struct TileAt {
-    int seq, tile, first, n;   // first: row of the sequence's first new token; n: its new tokens
-};
-__device__ inline int offset_of(const AttnLaunch& a, int i) { return max(0, min(a.q_offsets[i], int(a.total_q))); }
-__device__ bool find_tile(const AttnLaunch& a, int group, int rows, int flat, TileAt* at) {
-    const int lane = threadIdx.x & 63;
-    int before = 0;
-    for (int base = 0; base < a.num_seqs; base += 64) {
-        const int b = base + lane;
-        const int first = b < a.num_seqs ? offset_of(a, b) : 0;
-        const int n = b < a.num_seqs ? max(0, offset_of(a, b + 1) - first) : 0;
-        int upto = int((int64_t(n) * group + rows - 1) / rows);
-        const int own = upto;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int x = __shfl_up(upto, d);
-            if (lane >= d) upto += x;
-        }
-        const unsigned long long past = __ballot(flat < before + upto);
-        if (past) {
-            const int who = __builtin_ctzll(past);
-            at->seq = base + who;
-            at->tile = flat - before - __shfl(upto - own, who);
-            at->first = __shfl(first, who);
-            at->n = __shfl(n, who);
-            return true;
-        }
-        before += __shfl(upto, 63);
-    }
-    return false;
-}
-
-// What a tile's rows may see, and in how many units of work.
-struct Reach {
-    int len, start;     // keys of the sequence; key of its first new token
-    int end;            // keys that any row of the tile may see
-    int units;
-};
-__device__ inline Reach reach_of(const AttnLaunch& a, const TileAt& at, int group, int rows) {
-    Reach r;
-    const int64_t room = min(a.max_pages << a.c.log2_page, a.max_len);
-    r.len = int(max(int64_t(0), min(int64_t(a.lens[at.seq]), room)));
-    r.start = r.len - at.n;
-    const int last = min(at.n - 1, (at.tile * rows + rows - 1) / group);
-    r.end = a.mask ? r.len : max(0, min(r.len, r.start + last + 1));
-    const int chunks = (r.end + 63) / 64;
-    r.units = max(1, (chunks + a.chunks_per_unit - 1) / a.chunks_per_unit);
-    return r;
-}
-
-template <int D, int NT>
-struct PartialSize {
-    static constexpr int kRows = 16 * NT, kFloats = kRows * (D + 2);
-};
-
-template <int D, int ELEM, int NT>
-__global__ __launch_bounds__(kThreads) void attn_kernel(AttnLaunch a) {
-    constexpr int kRows = 16 * NT;
-    constexpr int kLoads = D * ELEM / 16;          // 1 KB loads of a chunk's keys, and of its values
+template <int D, int ELEM, int NT, int RG>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void attn_kernel(AttnLaunch a) {
+    constexpr int kRows = 16 * NT * RG;            // of the tile; a wave has 16 NT of them
+    constexpr int kKeyWaves = kWaves / RG;         // waves that share rows split the chunks
+    constexpr int kBlocks = 4 / ELEM;              // 16-key blocks of a chunk
+    constexpr int kKeys = 16 * kBlocks;
+    constexpr int kParts = NT == 2 && kBlocks == 4 ? 2 : 1;    // of a chunk, one after the other, for registers
+    constexpr int kLoads = D / 16;                 // 1 KB loads of a chunk's keys, and of its values
+    constexpr int kPer = kLoads / kBlocks;         // of a block's keys
     constexpr int kSteps = D / 32;                 // MFMA steps along the head
     constexpr int kPad = D + 4;
-    __shared__ float o_s[kRows * kPad];
-    __shared__ float m_s[kWaves][kRows], l_s[kWaves][kRows];
+    // 32 rows over 8-bit keys: the queries stay in LDS (which holds the results later), for registers
+    constexpr bool kQueriesInLds = NT == 2 && ELEM == 1 && D == 128;
+    __shared__ __attribute__((aligned(16))) float o_s[kRows * kPad];
+    __shared__ float m_s[kKeyWaves][kRows], l_s[kKeyWaves][kRows];
+    // rows' elements that an infinity (bit 0), -infinity (1) or NaN (2) among the values reaches: 4 bits each
+    __shared__ uint32_t odd_s[kRows * (D / 8)];
+    __shared__ int odd_any;
     const int heads = a.c.heads, group = a.q_heads / heads;
-    const int head = blockIdx.x % heads, rest = blockIdx.x / heads;
-    const int unit = rest % a.max_units, flat = rest / a.max_units;
-    TileAt at;
-    if (!find_tile(a, group, kRows, flat, &at)) return;
-    const Reach r = reach_of(a, at, group, kRows);
-    if (unit >= r.units) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
-
-    // this lane's rows: queries as the second operand of K Q^T, in the order of the keys' chunks
-    s16x8 q[NT][kSteps];
-    int sees[NT];                  // causal: keys below this one; tree: the row's mask words start here
-    bool valid[NT];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        const int row = at.tile * kRows + nt * 16 + col;
-        const int i = row / group;
-        valid[nt] = i < at.n;
-        sees[nt] = a.mask ? i : r.start + i + 1;
-        const uint16_t* qp = a.q + int64_t(at.first + (valid[nt] ? i : 0)) * a.ldq + int64_t(head * group + (valid[nt] ? row % group : 0)) * D;
-#pragma unroll
-        for (int f = 0; f < kSteps; ++f) {
-            const int d = ELEM == 1 ? (4 * (f / 2) + g) * 16 + f % 2 * 8 : (4 * f + g) * 8;
-            q[nt][f] = valid[nt] ? *reinterpret_cast<const s16x8*>(qp + d) : s16x8{0, 0, 0, 0, 0, 0, 0, 0};
-        }
+    const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
+    const int wave = uniform(int(threadIdx.x >> 6)), key_wave = wave % kKeyWaves, row0 = wave / kKeyWaves * (16 * NT);
+    const int log2_chunks = a.c.log2_page - a.log2_keys;       // chunks of a page
+    Seq s;
+    int64_t place, place_end, total = 0;
+    int groups = a.groups, me = blockIdx.x;
+    AttnShared* shared = reinterpret_cast<AttnShared*>(a.ws + attn_shared_at<D>(a.groups, kRows));
+    if (a.split) {
+        attn_find(a, 0, &s, &total);
+        groups = attn_groups(a, total);
+        if (me < groups) me = attn_by_xcd(me, groups);
+        if (threadIdx.x == 0) shared[me].last = -1;
+        if (me >= groups) return;
+        place = me * total / groups;
+        place_end = (me + 1) * total / groups;
+    } else {
+        place = me;
+        place_end = me + 1;
     }
-    // chunks below this one are seen whole by every row
-    const int whole = a.mask ? max(0, r.start) / 64 : max(0, min(r.len, r.start + at.tile * kRows / group + 1)) / 64;
+    const int64_t place0 = place;
+    for (int i = threadIdx.x; i < kRows * (D / 8); i += kThreads) odd_s[i] = 0;
+    if (threadIdx.x == 0) odd_any = 0;
+    __syncthreads();
+    while (place < place_end) {
+        if (!attn_find(a, place, &s, nullptr)) return;
+        // the piece: a tile's chunks [chunk0, chunk1)
+        const int64_t in_seq = place - s.before;
+        const int tile_of_seq = uniform(int(a.split ? in_seq / s.chunks : in_seq));
+        const int head = uniform(tile_of_seq / s.tiles), tile = tile_of_seq - head * s.tiles;
+        const int64_t tile_start = s.before + (a.split ? int64_t(tile_of_seq) * s.chunks : tile_of_seq);
+        const int chunk0 = uniform(a.split ? int(place - tile_start) : 0);
+        const int chunk1 = uniform(a.split ? int(min(int64_t(s.chunks), place_end - tile_start)) : s.chunks);
+        const bool whole = chunk0 == 0 && chunk1 == s.chunks;
+        const int64_t slot = 2 * int64_t(me) + (tile_start > place0 ? 1 : 0);
+        place = tile_start + (a.split ? chunk1 : 1);
+        if (a.split && tile_start >= place0 && chunk1 < s.chunks && threadIdx.x == 0)     // others go on with it
+            shared[me] = AttnShared{s.first, s.n, head, tile, attn_group_of(tile_start + s.chunks - 1, total, groups), int(slot)};
+        // keys below 'all' are seen by every row of the wave, keys from 'end' on by none
+        const int start = s.len - s.n, first_row = tile * kRows + row0;
+        const int all = uniform(max(0, min(s.len, a.mask ? start : start + first_row / group + 1)));
+        const int end = uniform(max(0, min(s.len, a.mask ? s.len : start + min(s.n - 1, (first_row + 16 * NT - 1) / group) + 1)));
+        const int chunk_end = first_row / group >= s.n ? 0 : min(chunk1, (end + kKeys - 1) / kKeys);
 
-    f32x4v o[NT][D / 16];
-    float m[NT], l[NT];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        m[nt] = -INFINITY;
-        l[nt] = 0.f;
-#pragma unroll
-        for (int db = 0; db < D / 16; ++db) o[nt][db] = f32x4v{0.f, 0.f, 0.f, 0.f};
-    }
-    const int chunk_end = min((unit + 1) * a.chunks_per_unit, (r.end + 63) / 64);
-    const int32_t* table = a.page_table + int64_t(at.seq) * a.max_pages;
-    const int log2_chunks = a.c.log2_page - 6;     // chunks of a page
-    for (int chunk = unit * a.chunks_per_unit + wave; chunk < chunk_end; chunk += kWaves) {
-        const int64_t page = table[chunk >> log2_chunks];
-        if (page < 0 || page >= a.c.num_pages) continue;       // a page that is none: keys that nobody sees
-        const int in_page = chunk & ((1 << log2_chunks) - 1);
-        const int64_t block = ((page * heads + head) << a.c.log2_page) + in_page * 64;   // first key, in tokens
-        const u32x4* kp = reinterpret_cast<const u32x4*>(a.c.k + block * (D * ELEM)) + lane;
-        const u32x4* vp = reinterpret_cast<const u32x4*>(a.c.v + block * (D * ELEM)) + lane;
-        u32x4 kw[kLoads], vw[kLoads];
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) kw[i] = kp[i * 64];
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) vw[i] = vp[i * 64];
-        uint32_t k_exp = 0;
-        u32x4 v_exp = {0, 0, 0, 0};
-        if (ELEM == 1) {
-            k_exp = *reinterpret_cast<const uint32_t*>(a.c.k_exp + block + col * 4);
-            v_exp = *reinterpret_cast<const u32x4*>(a.c.v_exp + block + g * 16);
-        }
-        // S^T: keys 16 mb + 4 g + i of the chunk, row col
-        f32x4v s[NT][4];
-#pragma unroll
-        for (int mb = 0; mb < 4; ++mb) {
-            s16x8 kf[kSteps];
-            if (ELEM == 1) {
-                const float scale = exp_scale(k_exp >> (8 * mb) & 0xff);
-#pragma unroll
-                for (int f = 0; f < kSteps; ++f) {
-                    const u32x4 w = kw[mb * (kLoads / 4) + f / 2];
-                    const uint32_t lo = w[f % 2 * 2], hi = w[f % 2 * 2 + 1];
-                    kf[f] = __builtin_bit_cast(s16x8, u32x4{fp8_to_bf16<false>(lo, scale), fp8_to_bf16<true>(lo, scale),
-                                                            fp8_to_bf16<false>(hi, scale), fp8_to_bf16<true>(hi, scale)});
-                }
-            } else {
-#pragma unroll
-                for (int f = 0; f < kSteps; ++f) kf[f] = __builtin_bit_cast(s16x8, kw[mb * (kLoads / 4) + f]);
-            }
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                s[nt][mb] = f32x4v{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int f = 0; f < kSteps; ++f)
-                    s[nt][mb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, kf[f]),
-                                                                       __builtin_bit_cast(bf16x8v, q[nt][f]), s[nt][mb], 0, 0, 0);
-            }
-        }
-        const bool masked = chunk >= whole;
-        uint32_t seen[NT];         // bit 4 mb + i
-        if (masked) {
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                seen[nt] = 0;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int key = chunk * 64 + (e >> 2) * 16 + 4 * g + (e & 3);
-                    bool ok = valid[nt] && key < r.len;
-                    if (a.mask) {
-                        const int j = key - r.start;
-                        if (j >= 0) {
-                            ok = ok && (j >> 5) < a.mask_words;
-                            if (ok) ok = a.mask[int64_t(at.first + sees[nt]) * a.mask_words + (j >> 5)] >> (j & 31) & 1;
-                        }
-                    } else {
-                        ok = ok && key < sees[nt];
-                    }
-                    seen[nt] |= uint32_t(ok) << e;
-                    if (!ok) s[nt][e >> 2][e & 3] = -INFINITY;
-                }
-            }
-        }
-        // running maximum and sum; P^T as bf16 operands of two 32-key steps
-        s16x8 p[NT][2];
+        // this lane's rows: queries as the second operand of K Q^T, in the order of the keys' chunks
+        u32x4 q[kQueriesInLds ? 1 : NT][kQueriesInLds ? 1 : kSteps];
+        u32x4* q_s = reinterpret_cast<u32x4*>(o_s) + row0 / 16 * kSteps * 64 + lane;
+        int own[NT];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            float top = -INFINITY;
+            const int row = first_row + nt * 16 + col;
+            own[nt] = row / group;
+            const bool valid = own[nt] < s.n;
+            const uint16_t* qp = a.q + int64_t(s.first + (valid ? own[nt] : 0)) * a.ldq + int64_t(head * group + (valid ? row - own[nt] * group : 0)) * D;
+            if (!valid) own[nt] = -1;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) top = fmaxf(top, s[nt][e >> 2][e & 3]);
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float next = fmaxf(m[nt], top * a.scale_log2);
-            const float base = next == -INFINITY ? 0.f : next;
-            const float shrink = __builtin_amdgcn_exp2f(m[nt] - base);
-            m[nt] = next;
-            float sum = 0.f, w[16];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[nt][e >> 2][e & 3], a.scale_log2, -base));
-                sum += x;
-                w[e] = x;
-                if (ELEM == 1) w[e] = x * exp_scale(v_exp[e >> 2] >> (8 * (e & 3)) & 0xff);
+            for (int f = 0; f < kSteps; ++f) {
+                const int d = ELEM == 1 ? (4 * (f / 2) + g) * 16 + f % 2 * 8 : (4 * f + g) * 8;
+                const u32x4 x = *reinterpret_cast<const u32x4*>(qp + d);       // rows past the end: the first one's, not stored
+                if (kQueriesInLds) q_s[(nt * kSteps + f) * 64] = x;            // waves that share rows write the same
+                else q[nt][f] = x;
             }
-            if (masked) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) w[e] = seen[nt] >> e & 1 ? w[e] : 0.f;    // a scale past the end may be anything
-            }
-            l[nt] = l[nt] * shrink + sum;
-#pragma unroll
-            for (int db = 0; db < D / 16; ++db) o[nt][db] *= shrink;
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                p[nt][h] = __builtin_bit_cast(s16x8, u32x4{pack_bf16(w[8 * h], w[8 * h + 1]), pack_bf16(w[8 * h + 2], w[8 * h + 3]),
-                                                           pack_bf16(w[8 * h + 4], w[8 * h + 5]), pack_bf16(w[8 * h + 6], w[8 * h + 7])});
         }
-        // O^T: elements 16 db + 4 g + i of the head, row col
-        const int left = r.len - chunk * 64 - 4 * g;       // this lane's key 16 mb + i exists where that is below left
+        f32x4v o[NT][D / 16];
+        float m[NT], l[NT];
 #pragma unroll
-        for (int db = 0; db < D / 16; ++db) {
+        for (int nt = 0; nt < NT; ++nt) {
+            m[nt] = -INFINITY;
+            l[nt] = 0.f;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                u32x4 vf;
-                if (ELEM == 1) {
-                    const u32x4 w = vw[db];
-                    vf = u32x4{fp8_to_bf16<false>(w[2 * h], 1.f), fp8_to_bf16<true>(w[2 * h], 1.f),
-                               fp8_to_bf16<false>(w[2 * h + 1], 1.f), fp8_to_bf16<true>(w[2 * h + 1], 1.f)};
-                } else {
-                    vf = vw[h * (D / 16) + db];
-                }
-                u32x4 special = {0, 0, 0, 0};              // bf16 elements that are no finite numbers
-                if (masked) {
-                    bool any = false;
+            for (int db = 0; db < D / 16; ++db) o[nt][db] = f32x4v{0.f, 0.f, 0.f, 0.f};
+        }
+        // a chunk's first key in the pool, in tokens; negative: a page that is none
+        const ConstInts table = ConstInts(a.page_table + int64_t(s.seq) * a.max_pages);
+        const int num_pages = int(a.c.num_pages), page_tokens = heads << a.c.log2_page, head_at = head << a.c.log2_page;
+        const int in_page = (1 << log2_chunks) - 1;
+        auto page_at = [&](int chunk) { return chunk < chunk_end ? table[chunk >> log2_chunks] : -1; };
+        auto block_of = [&](int chunk, int page) -> int64_t {
+            return page < 0 || page >= num_pages ? -1 : int64_t(page) * page_tokens + (head_at + (chunk & in_page) * kKeys);
+        };
+        // Keys of the next chunk are loaded under this one's softmax and second product, its values under the next one's
+        // first, page numbers a chunk earlier.  Past the end (and for pages that are none) a block that exists is loaded.
+        u32x4 kw[kBlocks][kPer], vw[kLoads], v_exp = {0, 0, 0, 0};
+        uint32_t k_exp = 0;
+        auto load_keys = [&](int64_t block) {
+            const u32x4* p = reinterpret_cast<const u32x4*>(a.c.k + max(block, int64_t(0)) * (D * ELEM)) + lane;
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const int k0 = (2 * h + (x >> 1)) * 16 + (x & 1) * 2;
-                        vf[x] &= (k0 < left ? 0xffffu : 0u) | (k0 + 1 < left ? 0xffff0000u : 0u);
-                        const uint32_t hit = ((vf[x] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((vf[x] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
-                        special[x] = vf[x] & hit;
-                        vf[x] &= ~hit;
-                        any |= hit != 0;
-                    }
-                    if (__ballot(any)) {
-                        // 0 * NaN would reach rows that do not see the key: infinities and NaNs
-                        // go in one kind at a time, to the rows that see one
-#pragma unroll 1
-                        for (int kind = 0; kind < 3; ++kind) {
-                            u32x4 is;
+            for (int i = 0; i < kLoads; ++i) kw[i / kPer][i % kPer] = RG == 1 ? __builtin_nontemporal_load(p + i * 64) : p[i * 64];
+            if (ELEM == 1) k_exp = *reinterpret_cast<const uint32_t*>(a.c.k_exp + max(block, int64_t(0)) + col * 4);
+        };
+        auto load_values = [&](int64_t block) {
+            const u32x4* p = reinterpret_cast<const u32x4*>(a.c.v + max(block, int64_t(0)) * (D * ELEM)) + lane;
 #pragma unroll
-                            for (int x = 0; x < 4; ++x) {
-                                const uint32_t lo = special[x] & 0xffffu, hi = special[x] >> 16;
-                                const bool a0 = kind == 0 ? lo == 0x7f80u : kind == 1 ? lo == 0xff80u : (lo & 0x7fu) != 0;
-                                const bool a1 = kind == 0 ? hi == 0x7f80u : kind == 1 ? hi == 0xff80u : (hi & 0x7fu) != 0;
-                                is[x] = (a0 ? 0x3f80u : 0u) | (a1 ? 0x3f800000u : 0u);
-                            }
-                            const float add = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
+            for (int i = 0; i < kLoads; ++i) vw[i] = RG == 1 ? __builtin_nontemporal_load(p + i * 64) : p[i * 64];
+            if (ELEM == 1) v_exp = *reinterpret_cast<const u32x4*>(a.c.v_exp + max(block, int64_t(0)) + g * 16);
+        };
+        // a 32-key operand of O^T = V^T P^T: half h of an 8-bit load's 16 keys, or a whole 16-bit load
+        auto value_of = [&](int db, int h) {
+            const u32x4 w = vw[db];
+            if (ELEM == 2) return w;
+            return u32x4{fp8_to_bf16<false>(w[2 * h], 1.f), fp8_to_bf16<true>(w[2 * h], 1.f),
+                         fp8_to_bf16<false>(w[2 * h + 1], 1.f), fp8_to_bf16<true>(w[2 * h + 1], 1.f)};
+        };
+        int chunk = chunk0 + key_wave;
+        int64_t block = block_of(chunk, page_at(chunk)), next = -1;
+        int next_page = page_at(chunk + kKeyWaves);
+        uint32_t odd = 0;
+        if (chunk < chunk_end) {
+            load_keys(block);
+            load_values(block);
+        }
+        auto step = [&](auto is_masked) {
+            constexpr bool masked = decltype(is_masked)::value;
+            const int left = block < 0 ? 0 : s.len - chunk * kKeys - 4 * g;        // this lane's key 16 mb + i exists below that
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) {
-                                u32x4 ones;
-#pragma unroll
-                                for (int x = 0; x < 4; ++x) {
-                                    const uint32_t two = seen[nt] >> (8 * h + 2 * x) & 3;
-                                    ones[x] = (two & 1 ? 0x3f80u : 0u) | (two & 2 ? 0x3f800000u : 0u);
-                                }
-                                const f32x4v hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, is),
-                                                                                           __builtin_bit_cast(bf16x8v, ones), f32x4v{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-                                for (int i = 0; i < 4; ++i)
-                                    if (hits[i] > 0.f) o[nt][db][i] += add;
-                            }
-                        }
-                    }
-                }
+            for (int part = 0; part < kParts; ++part) {
+                // S^T: keys 16 mb + 4 g + i of the chunk, row col
+                constexpr int kB = kBlocks / kParts;
+                const int mb0 = part * kB;
+                f32x4v x[NT][kB];
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
-                    o[nt][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, vf),
-                                                                       __builtin_bit_cast(bf16x8v, p[nt][h]), o[nt][db], 0, 0, 0);
+#pragma unroll
+                    for (int mb = 0; mb < kB; ++mb) x[nt][mb] = f32x4v{0.f, 0.f, 0.f, 0.f};
+                if (kQueriesInLds) asm volatile("" ::: "memory");              // read them again for every part
+#pragma unroll
+                for (int f = 0; f < kSteps; ++f) {
+                    u32x4 qf[NT];
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) qf[nt] = kQueriesInLds ? q_s[(nt * kSteps + f) * 64] : q[kQueriesInLds ? 0 : nt][kQueriesInLds ? 0 : f];
+#pragma unroll
+                    for (int mb = 0; mb < kB; ++mb) {
+                        u32x4 kf;
+                        if (ELEM == 1) {
+                            const float scale = exp_scale(k_exp >> (8 * (mb0 + mb)) & 0xff);
+                            const uint32_t lo = kw[mb0 + mb][f / 2][f % 2 * 2], hi = kw[mb0 + mb][f / 2][f % 2 * 2 + 1];
+                            kf = u32x4{fp8_to_bf16<false>(lo, scale), fp8_to_bf16<true>(lo, scale), fp8_to_bf16<false>(hi, scale), fp8_to_bf16<true>(hi, scale)};
+                        } else {
+                            kf = kw[mb0 + mb][f];
+                        }
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) x[nt][mb] = mfma_16x16x32(kf, qf[nt], x[nt][mb]);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                if (!masked && part == kParts - 1) load_keys(next);
+                if (masked) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        const uint32_t seen = own[nt] >= 0 ? attn_seen<kB>(a, s, own[nt], chunk * kKeys + 16 * mb0 + 4 * g - start, left - 16 * mb0) : 0u;
+#pragma unroll
+                        for (int e = 0; e < 4 * kB; ++e) x[nt][e >> 2][e & 3] = seen >> e & 1 ? x[nt][e >> 2][e & 3] : -INFINITY;
+                    }
+                    // entries past the end may be anything: their scales and values count as 0.  So do infinities and NaNs
+                    // among the others for now: 0 * NaN would reach rows that do not see the key
+                    if (part == 0) {
+#pragma unroll
+                        for (int mb = 0; mb < kBlocks; ++mb) v_exp[mb] &= attn_first_bytes(left - 16 * mb);
+#pragma unroll
+                        for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                vw[i][j] &= ELEM == 1 ? attn_first_bytes(left - 16 * j) : attn_first_halves(left - 16 * (j >> 1) - 2 * (j & 1));
+                                const uint32_t bad = attn_odd<ELEM>(vw[i][j]);
+                                vw[i][j] &= ~bad;
+                                odd |= bad;
+                            }
+                    }
+                }
+                if (!masked && block < 0) continue;        // a page that is none: keys that nobody sees
+                // running maximum and sum, P^T (times the values' scales) as operands of 32-key steps.  The sums are
+                // relative to an m up to kSlack below the maximum (a factor of at most 2^kSlack), so that they need
+                // rescaling only when the maximum has grown by that
+                u32x4 p[NT][kB / 2];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    float top = -INFINITY;
+#pragma unroll
+                    for (int e = 0; e < 4 * kB; ++e) top = fmaxf(top, x[nt][e >> 2][e & 3]);
+                    top = fmaxf(top, __shfl_xor(top, 16));
+                    top = fmaxf(top, __shfl_xor(top, 32));
+                    const float want = top * a.scale_log2;
+                    if (__ballot(want > m[nt] + kSlack)) {
+                        const float grown = fmaxf(m[nt], want);
+                        const float shrink = __builtin_amdgcn_exp2f(m[nt] - (grown == -INFINITY ? 0.f : grown));
+                        m[nt] = grown;
+                        l[nt] *= shrink;
+#pragma unroll
+                        for (int db = 0; db < D / 16; ++db) o[nt][db] *= shrink;
+                    }
+                    const float base = m[nt] == -INFINITY ? 0.f : m[nt];
+#pragma unroll
+                    for (int h = 0; h < kB / 2; ++h) {
+                        float w[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(x[nt][2 * h + (e >> 2)][e & 3], a.scale_log2, -base));
+                            l[nt] += y;
+                            w[e] = ELEM == 1 ? y * exp_scale(v_exp[mb0 + 2 * h + (e >> 2)] >> (8 * (e & 3)) & 0xff) : y;
+                        }
+                        p[nt][h] = u32x4{pack_bf16(w[0], w[1]), pack_bf16(w[2], w[3]), pack_bf16(w[4], w[5]), pack_bf16(w[6], w[7])};
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                // O^T: elements 16 db + 4 g + i of the head, row col
+#pragma unroll
+                for (int db = 0; db < D / 16; ++db)
+#pragma unroll
+                    for (int h = 0; h < kB / 2; ++h) {
+                        const u32x4 vf = value_of(db, mb0 / 2 + h);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) o[nt][db] = mfma_16x16x32(vf, p[nt][h], o[nt][db]);
+                    }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (masked) load_keys(next);
+            load_values(next);
+        };
+        // chunks that the wave's rows see whole, then the others
+        auto run = [&](auto is_masked, int before) {
+            for (; chunk < before; chunk += kKeyWaves) {
+                next = block_of(chunk + kKeyWaves, next_page);
+                next_page = page_at(chunk + 2 * kKeyWaves);
+                step(is_masked);
+                block = next;
+            }
+        };
+        run(std::false_type(), min(chunk_end, all / kKeys));
+        run(std::true_type(), chunk_end);
+
+        // join the waves that share rows
+        if (__ballot(odd) && lane == 0) odd_any = 1;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            l[nt] += __shfl_xor(l[nt], 16);
+            l[nt] += __shfl_xor(l[nt], 32);
+            if (g == 0) {
+                m_s[key_wave][row0 + nt * 16 + col] = m[nt];
+                l_s[key_wave][row0 + nt * 16 + col] = l[nt];
             }
         }
-    }
-
-    // join the waves
+        __syncthreads();
+        for (int w = 0; w < kKeyWaves; ++w) {
+            if (key_wave == w) {
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        l[nt] += __shfl_xor(l[nt], 16);
-        l[nt] += __shfl_xor(l[nt], 32);
-        if (g == 0) {
-            m_s[wave][nt * 16 + col] = m[nt];
-            l_s[wave][nt * 16 + col] = l[nt];
+                for (int nt = 0; nt < NT; ++nt) {
+                    const int row = row0 + nt * 16 + col;
+                    float top = m_s[0][row];
+#pragma unroll
+                    for (int i = 1; i < kKeyWaves; ++i) top = fmaxf(top, m_s[i][row]);
+                    const float f = __builtin_amdgcn_exp2f(m[nt] - (top == -INFINITY ? 0.f : top));
+#pragma unroll
+                    for (int db = 0; db < D / 16; ++db) {
+                        f32x4v* to = reinterpret_cast<f32x4v*>(o_s + row * kPad + db * 16 + 4 * g);
+                        // a wave without keys adds nothing (its m is -infinity: f and o are 0)
+                        *to = w ? *to + o[nt][db] * f : o[nt][db] * f;
+                    }
+                }
+            }
+            __syncthreads();
         }
-    }
-    __syncthreads();
-    for (int w = 0; w < kWaves; ++w) {
-        if (wave == w) {
+        if (odd_any) {
+            // infinities and NaNs among the values go in by themselves, one kind at a time, to the rows that see one
+            for (int c = chunk0 + key_wave; c < chunk_end; c += kKeyWaves) {
+                const int64_t at = block_of(c, page_at(c));
+                if (c * kKeys + kKeys <= all || at < 0) continue;
+                const int left = s.len - c * kKeys - 4 * g;
+#pragma unroll 1
+                for (int nt = 0; nt < NT; ++nt) {
+                    const int row = row0 + nt * 16 + col, i = (tile * kRows + row) / group;
+                    const uint32_t seen = i < s.n ? attn_seen<kBlocks>(a, s, i, c * kKeys + 4 * g - start, left) : 0u;
+#pragma unroll 1
+                    for (int step = 0; step < 3 * (D / 16) * (kBlocks / 2); ++step) {
+                        const int kind = step % 3, db = step / 3 % (D / 16), h = step / 3 / (D / 16);
+                        u32x4 vf = reinterpret_cast<const u32x4*>(a.c.v + at * (D * ELEM))[db * 64 + lane], is, ones;
+                        if (ELEM == 1) {
+                            const uint32_t lo = h ? vf[2] : vf[0], hi = h ? vf[3] : vf[1];
+                            vf = u32x4{fp8_to_bf16<false>(lo, 1.f), fp8_to_bf16<true>(lo, 1.f), fp8_to_bf16<false>(hi, 1.f), fp8_to_bf16<true>(hi, 1.f)};
+                        }
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                const int row = nt * 16 + col;
-                float top = m_s[0][row];
+                        for (int j = 0; j < 4; ++j) {
+                            vf[j] &= attn_first_halves(left - 32 * h - 16 * (j >> 1) - 2 * (j & 1));
+                            is[j] = attn_special(vf[j] & 0xffffu, kind) | attn_special(vf[j] >> 16, kind) << 16;
+                            const uint32_t two = seen >> (8 * h + 2 * j);
+                            ones[j] = (two & 1 ? 0x3f80u : 0u) | (two & 2 ? 0x3f800000u : 0u);
+                        }
+                        const f32x4v hits = mfma_16x16x32(is, ones, f32x4v{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-                for (int x = 1; x < kWaves; ++x) top = fmaxf(top, m_s[x][row]);
-                const float f = __builtin_amdgcn_exp2f(m[nt] - (top == -INFINITY ? 0.f : top));
+                        for (int j = 0; j < 4; ++j)     // elements 16 db + 4 g + j of the row: 4 bits each
+                            if (hits[j] > 0.f) atomicOr(&odd_s[row * (D / 8) + db * 2 + (g >> 1)], 1u << (16 * (g & 1) + 4 * j + kind));
+                    }
+                }
+            }
+            __syncthreads();
+        }
+        for (int u = threadIdx.x; u < kRows * (D / 8); u += kThreads) {
+            const int row = u / (D / 8), d = u % (D / 8) * 8;
+            const int at = tile * kRows + row, i = at / group;
+            if (i >= s.n) continue;
+            float top = m_s[0][row], sum = 0.f;
 #pragma unroll
-                for (int db = 0; db < D / 16; ++db) {
-                    f32x4v* to = reinterpret_cast<f32x4v*>(o_s + row * kPad + db * 16 + 4 * g);
-                    // a wave without keys adds nothing (its m is -infinity: f and o are 0)
-                    *to = w ? *to + o[nt][db] * f : o[nt][db] * f;
+            for (int w = 1; w < kKeyWaves; ++w) top = fmaxf(top, m_s[w][row]);
+#pragma unroll
+            for (int w = 0; w < kKeyWaves; ++w) sum += l_s[w][row] * __builtin_amdgcn_exp2f(m_s[w][row] - (top == -INFINITY ? 0.f : top));
+            float* from = o_s + row * kPad + d;
+            if (odd_any) {
+                const uint32_t odd = odd_s[row * (D / 8) + d / 8];
+                for (int j = 0; j < 8; ++j) {
+                    if (odd >> (4 * j) & 1) from[j] += INFINITY;
+                    if (odd >> (4 * j) & 2) from[j] -= INFINITY;
+                    if (odd >> (4 * j) & 4) from[j] = NAN;
+                }
+            }
+            if (whole) {
+                const float inv = sum == 0.f ? 0.f : 1.f / sum;    // a row that sees no key: zeros
+                u32x4 w;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[j] = pack_bf16(from[2 * j] * inv, from[2 * j + 1] * inv);
+                *reinterpret_cast<u32x4*>(a.out + (int64_t(s.first + i) * a.q_heads + head * group + at - i * group) * D + d) = w;
+            } else {
+                float* part = a.ws + slot * attn_partial_floats<D>(kRows);
+#pragma unroll
+                for (int j = 0; j < 8; j += 4)
+                    *reinterpret_cast<f32x4v*>(part + row * D + d + j) = *reinterpret_cast<const f32x4v*>(from + j);
+                if (d == 0) {
+                    part[kRows * D + row] = top;
+                    part[kRows * D + kRows + row] = sum;
                 }
             }
         }
         __syncthreads();
-    }
-    for (int u = threadIdx.x; u < kRows * (D / 8); u += kThreads) {
-        const int row = u / (D / 8), d = u % (D / 8) * 8;
-        const int all = at.tile * kRows + row, i = all / group;
-        if (i >= at.n) continue;
-        float top = m_s[0][row], sum = 0.f;
-#pragma unroll
-        for (int x = 1; x < kWaves; ++x) top = fmaxf(top, m_s[x][row]);
-#pragma unroll
-        for (int x = 0; x < kWaves; ++x) sum += l_s[x][row] * __builtin_amdgcn_exp2f(m_s[x][row] - (top == -INFINITY ? 0.f : top));
-        const float* from = o_s + row * kPad + d;
-        if (r.units == 1) {
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;    // a row that sees no key: zeros
-            u32x4 w;
-#pragma unroll
-            for (int x = 0; x < 4; ++x) w[x] = pack_bf16(from[2 * x] * inv, from[2 * x + 1] * inv);
-            *reinterpret_cast<u32x4*>(a.out + (int64_t(at.first + i) * a.q_heads + head * group + all % group) * D + d) = w;
-        } else {
-            float* part = a.ws + ((int64_t(flat) * heads + head) * a.max_units + unit) * PartialSize<D, NT>::kFloats;
-#pragma unroll
-            for (int x = 0; x < 8; x += 4)
-                *reinterpret_cast<f32x4v*>(part + row * D + d + x) = *reinterpret_cast<const f32x4v*>(from + x);
-            if (d == 0) {
-                part[kRows * D + row] = top;
-                part[kRows * D + kRows + row] = sum;
-            }
+        if (odd_any) {          // uniform
+            for (int i = threadIdx.x; i < kRows * (D / 8); i += kThreads) odd_s[i] = 0;
+            __syncthreads();
+            if (threadIdx.x == 0) odd_any = 0;
+            __syncthreads();
         }
     }
 }
 
-// Joins the units of tiles that have several, in their order.
-template <int D, int NT>
+// Joins the partial results of the tile that begins in workgroup blockIdx.x of
+// the first launch and ends in a later one, in their order: ROWS rows of it, a
+// thread for eight elements, the parts dealt to groups of threads.
+template <int D, int ROWS>
 __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnLaunch a) {
-    constexpr int kRows = 16 * NT, kFloats = PartialSize<D, NT>::kFloats;
-    const int heads = a.c.heads, group = a.q_heads / heads;
-    const int head = blockIdx.x % heads, flat = blockIdx.x / heads;
-    TileAt at;
-    if (!find_tile(a, group, kRows, flat, &at)) return;
-    const Reach r = reach_of(a, at, group, kRows);
-    if (r.units == 1) return;
-    const float* parts = a.ws + (int64_t(flat) * heads + head) * a.max_units * kFloats;
-    for (int u = threadIdx.x; u < kRows * (D / 8); u += kThreads) {
-        const int row = u / (D / 8), d = u % (D / 8) * 8;
-        const int all = at.tile * kRows + row, i = all / group;
-        if (i >= at.n) continue;
-        float top = -INFINITY, sum = 0.f, o[8];
-        for (int x = 0; x < r.units; ++x) top = fmaxf(top, parts[int64_t(x) * kFloats + kRows * D + row]);
-        const float base = top == -INFINITY ? 0.f : top;
+    constexpr int kCols = D / 8, kParts = kThreads / (ROWS * kCols);
+    __shared__ float o_s[kParts][ROWS][D];
+    __shared__ float m_s[kParts][ROWS], l_s[kParts][ROWS];
+    const AttnShared t = reinterpret_cast<const AttnShared*>(a.ws + attn_shared_at<D>(a.groups, a.rows))[blockIdx.x];
+    const int group = a.q_heads / a.c.heads, floats = attn_partial_floats<D>(a.rows);
+    const int c = threadIdx.x % kCols * 8, j = threadIdx.x / kCols % ROWS, part = threadIdx.x / (kCols * ROWS);
+    const int row = blockIdx.y * ROWS + j, all_row = t.tile * a.rows + row, own = all_row / group;
+    if (t.last < 0 || (t.tile * a.rows + int(blockIdx.y) * ROWS) / group >= t.n) return;
+    float top = -INFINITY, sum = 0.f, o[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) o[j] = 0.f;
-        for (int x = 0; x < r.units; ++x) {
-            const float* part = parts + int64_t(x) * kFloats;
-            const float f = __builtin_amdgcn_exp2f(part[kRows * D + row] - base);
-            sum += f * part[kRows * D + kRows + row];
-            const f32x4v lo = *reinterpret_cast<const f32x4v*>(part + row * D + d), hi = *reinterpret_cast<const f32x4v*>(part + row * D + d + 4);
+    for (int i = 0; i < 8; ++i) o[i] = 0.f;
+    if (own < t.n) {
+#pragma unroll 4
+        for (int w = blockIdx.x + part; w <= t.last; w += kParts) {
+            const float* p = a.ws + (w == int(blockIdx.x) ? t.slot : 2 * int64_t(w)) * floats;
+            const float m = p[a.rows * D + row], l = p[a.rows * D + a.rows + row];
+            const f32x4v lo = *reinterpret_cast<const f32x4v*>(p + row * D + c), hi = *reinterpret_cast<const f32x4v*>(p + row * D + c + 4);
+            const float next = fmaxf(top, m), base = next == -INFINITY ? 0.f : next;
+            const float f = __builtin_amdgcn_exp2f(top - base), h = __builtin_amdgcn_exp2f(m - base);
+            top = next;
+            sum = sum * f + l * h;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) o[j] += f * lo[j], o[4 + j] += f * hi[j];
+            for (int i = 0; i < 4; ++i) o[i] = o[i] * f + lo[i] * h, o[4 + i] = o[4 + i] * f + hi[i] * h;
         }
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        u32x4 w;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) w[x] = pack_bf16(o[2 * x] * inv, o[2 * x + 1] * inv);
-        *reinterpret_cast<u32x4*>(a.out + (int64_t(at.first + i) * a.q_heads + head * group + all % group) * D + d) = w;
     }
+    if (kParts > 1) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o_s[part][j][c + i] = o[i];
+        if (c == 0) {
+            m_s[part][j] = top;
+            l_s[part][j] = sum;
+        }
+        __syncthreads();
+        if (part != 0) return;
+        for (int x = 1; x < kParts; ++x) {
+            const float next = fmaxf(top, m_s[x][j]), base = next == -INFINITY ? 0.f : next;
+            const float f = __builtin_amdgcn_exp2f(top - base), h = __builtin_amdgcn_exp2f(m_s[x][j] - base);
+            top = next;
+            sum = sum * f + l_s[x][j] * h;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o[i] = o[i] * f + o_s[x][j][c + i] * h;
+        }
+    }
+    if (own >= t.n) return;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = pack_bf16(o[2 * i] * inv, o[2 * i + 1] * inv);
+    *reinterpret_cast<u32x4*>(a.out + (int64_t(t.first + own) * a.q_heads + t.head * group + all_row - own * group) * D + c) = w;
 }
 
-template <int D, int ELEM, int NT>
+template <int D, int ELEM, int NT, int RG>
 hipError_t attn_as(const AttnLaunch& a, hipStream_t stream) {
-    const uint32_t tiles = uint32_t(a.max_tiles) * a.c.heads;
-    hipLaunchKernelGGL((attn_kernel<D, ELEM, NT>), dim3(tiles * a.max_units), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((attn_kernel<D, ELEM, NT, RG>), dim3(a.groups), dim3(kThreads), 0, stream, a);
     hipError_t e = hipGetLastError();
-    if (e == hipSuccess && a.max_units > 1) {
-        hipLaunchKernelGGL((attn_join_kernel<D, NT>), dim3(tiles), dim3(kThreads), 0, stream, a);
+    if (e == hipSuccess && a.split) {
+        // few rows: their tiles are few too, with many parts each
+        if (a.rows <= 64) hipLaunchKernelGGL((attn_join_kernel<D, 4>), dim3(a.groups, a.rows / 4), dim3(kThreads), 0, stream, a);
+        else hipLaunchKernelGGL((attn_join_kernel<D, 16>), dim3(a.groups, a.rows / 16), dim3(kThreads), 0, stream, a);
         e = hipGetLastError();
     }
     return e;
@@ -407,7 +456,12 @@ hipError_t attn_as(const AttnLaunch& a, hipStream_t stream) {
 
 template <int D, int ELEM>
 hipError_t attn_rows(const AttnLaunch& a, hipStream_t stream) {
-    return a.rows == 16 ? attn_as<D, ELEM, 1>(a, stream) : a.rows == 32 ? attn_as<D, ELEM, 2>(a, stream) : attn_as<D, ELEM, 4>(a, stream);
+    switch (a.rows) {
+        case 16: return attn_as<D, ELEM, 1, 1>(a, stream);
+        case 32: return attn_as<D, ELEM, 2, 1>(a, stream);
+        case 64: return attn_as<D, ELEM, 2, 2>(a, stream);
+        default: return attn_as<D, ELEM, 2, 4>(a, stream);
+    }
 }
 
 }  // namespace

@@ -60,19 +60,19 @@ int64_t span(int64_t rows, int64_t ld, int64_t width, int64_t elem) { return row
 
 }  // namespace
 
-// Rows per workgroup: the fewest of 16, 32 and 64 that hold a sequence's rows
-// of one key head.  Units of keys: as many as give about kTargetWorkgroups
-// workgroups, each at least one chunk per wave long.
-int64_t plan_attn(AttnLaunch* a, int head_dim, int) {
-    constexpr int64_t kTargetWorkgroups = 2048;
+// Rows per tile: the fewest of 16, 32, 64 and 128 that hold a sequence's rows
+// of one key head.  Keys are split where the tiles are too few to keep the CUs
+// evenly busy, unless no sequence has more than kWholeKeys keys: joining the
+// partial results costs a second launch.
+int64_t plan_attn(AttnLaunch* a, int head_dim, int elem_bytes) {
+    constexpr int64_t kSlots = 2 * 256, kWholeKeys = 1024;
     const int64_t group = a->q_heads / a->c.heads, most = a->max_q * group;
-    a->rows = most <= 16 ? 16 : most <= 32 ? 32 : 64;
-    a->max_tiles = std::min(a->num_seqs * ((most + a->rows - 1) / a->rows), a->total_q * group / a->rows + a->num_seqs);
-    const int64_t chunks = std::max<int64_t>(1, (a->max_len + 63) / 64), tiles = a->max_tiles * a->c.heads;
-    const int64_t units = std::max<int64_t>(1, std::min((chunks + 3) / 4, (kTargetWorkgroups + tiles - 1) / tiles));
-    a->chunks_per_unit = int(((chunks + units - 1) / units + 3) / 4 * 4);
-    a->max_units = int((chunks + a->chunks_per_unit - 1) / a->chunks_per_unit);
-    return a->max_units > 1 ? tiles * a->max_units * a->rows * (head_dim + 2) : 0;
+    a->rows = most <= 16 ? 16 : most <= 32 ? 32 : most <= 64 ? 64 : 128;
+    a->log2_keys = elem_bytes == 1 ? 6 : 5;
+    a->max_tiles = std::min(a->num_seqs * ((most + a->rows - 1) / a->rows), a->total_q * group / a->rows + a->num_seqs) * a->c.heads;
+    a->split = a->max_tiles < 4 * kSlots && a->max_len > kWholeKeys;
+    a->groups = int(a->split ? kSlots : std::min<int64_t>(a->max_tiles, kMaxGrid));
+    return a->split ? 2 * a->groups * int64_t(a->rows) * (head_dim + 2) + a->groups * 8 : 0;
 }
 
 }  // namespace tl
@@ -223,7 +223,7 @@ int tl_attn(const void* Q, int64_t ldq, const tl_kv_cache* cache, const int32_t*
     a.scale_log2 = scale * 1.44269504088896340736f;
     a.out = static_cast<uint16_t*>(O);
     const int64_t floats = plan_attn(&a, D, cache->elem_bytes);
-    if (a.max_tiles * a.c.heads > kMaxGrid / a.max_units) return TL_EUNSUPPORTED;
+    if (a.max_tiles > kMaxGrid) return TL_EUNSUPPORTED;
     std::shared_ptr<void> keep;
     if (floats > 0) {
         void* ws = nullptr;

@@ -92,11 +92,14 @@ struct AttnLaunch {
     int q_heads;
     float scale_log2;         // scale * log2(e)
     uint16_t* out;
-    // the plan: rows per tile, tiles (an upper bound over all sequences), keys
-    // per unit of work in 64-key chunks, and units per tile (an upper bound)
-    int rows, chunks_per_unit, max_units;
+    // the plan: rows per tile, keys per chunk (a power of two), tiles of all
+    // sequences and heads (an upper bound), whether keys are split over
+    // workgroups, and how many of those
+    int rows, log2_keys;
+    bool split;
     int64_t max_tiles;
-    float* ws;                // partial results (max_units > 1)
+    int groups;
+    float* ws;                // partial results: two per workgroup (split)
 };
 // Fills the plan; returns the workspace it needs, in floats.
 int64_t plan_attn(AttnLaunch* a, int head_dim, int elem_bytes);
