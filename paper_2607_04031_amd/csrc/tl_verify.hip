@@ -19,8 +19,9 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWalkThreads = 1024;
-constexpr int kMaxRanges = 32;
-constexpr int kMinRange = 4096;
+constexpr int kAtOnce = 8;                          // elements of a lane's load
+constexpr int kMinRange = kThreads * kAtOnce;       // one load of each lane
+constexpr int kMaxRanges = 64;                      // one lane joins each
 constexpr float kLog2e = 1.44269504088896340736f;
 
 struct RowStat {
@@ -35,19 +36,22 @@ struct Last {           // what walk leaves for sample
     int first;
     unsigned arrived;
 };
-struct Best {
-    float rest, all;    // largest weight / noise of what is left, and of the whole distribution
-    int rest_at, all_at;
+struct Best {           // largest weight / noise of what is left, and of the whole distribution
+    float rest;
+    int rest_at;
+    float all;
+    int all_at;
 };
+typedef unsigned long long u64x2 __attribute__((ext_vector_type(2)));
 
 struct Params {
     VerifyLaunch a;
-    int ranges;         // of a row, in stats and in sample
-    int64_t range;      // elements, a multiple of 8
+    int ranges, sample_ranges;      // of a row, in stats and in sample
+    int64_t range, sample_range;    // their elements, multiples of kMinRange
     RowStat* stats;     // [total][ranges]
     Last* last;         // [num_seqs]
-    Best* best;         // [num_seqs][ranges]
-    float* mass;        // [num_seqs][max_nodes]: sum left before each tried child
+    Best* best;         // [num_seqs][sample_ranges]
+    float* mass;        // [num_seqs][max_nodes]: 1 / sum left before each tried child
     int32_t* tried;     // [num_seqs][max_nodes]: the tried children's tokens
 };
 
@@ -62,16 +66,22 @@ __device__ inline float load_one(const void* p, int64_t at) {
     return static_cast<const float*>(p)[at];
 }
 
-// four elements from any element's address
+// eight elements from any element's address
 template <bool BF16>
-__device__ inline void load_four(const void* p, int64_t at, float (&x)[4]) {
+__device__ inline void load_eight(const void* p, int64_t at, float (&x)[8]) {
     if (BF16) {
-        u32x2 w;
-        __builtin_memcpy(&w, static_cast<const uint16_t*>(p) + at, 8);
-        x[0] = bf16_lo(w[0]), x[1] = bf16_hi(w[0]), x[2] = bf16_lo(w[1]), x[3] = bf16_hi(w[1]);
+        u32x4 w;
+        __builtin_memcpy(&w, static_cast<const uint16_t*>(p) + at, 16);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[2 * j] = bf16_lo(w[j]), x[2 * j + 1] = bf16_hi(w[j]);
     } else {
-        __builtin_memcpy(x, static_cast<const float*>(p) + at, 16);
+        __builtin_memcpy(x, static_cast<const float*>(p) + at, 32);
     }
+}
+template <bool BF16>
+__device__ inline void load_some(const void* p, int64_t at, int some, float fill, float (&x)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = j < some ? load_one<BF16>(p, at + j) : fill;
 }
 
 __device__ inline void take(float& v, int& at, float w, int j) {
@@ -99,38 +109,55 @@ __global__ __launch_bounds__(kThreads) void verify_stats_kernel(Params p) {
     const int64_t row = blockIdx.x / p.ranges;
     const int range = blockIdx.x - int(row * p.ranges);
     const int64_t V = p.a.vocab, from = range * p.range, to = min(V, from + p.range);
+    constexpr int kAhead = 4;                       // loads in flight, the first of them before the temperature is known
+    const int64_t base = row * V, last = to - (kAhead - 1) * kMinRange - kAtOnce;
+    int64_t v = from + threadIdx.x * kAtOnce;
+    float x[kAhead][8];
+    auto load = [&](int64_t v) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) load_eight<BF16>(p.a.logits, base + v + u * kMinRange, x[u]);
+    };
+    if (v <= last) load(v);
     // the row's sequence: how many sequences begin at or before it
-    __shared__ int seq_s;
-    if (threadIdx.x < 64) {
-        int seq = -1;
-        for (int b = 0; b < p.a.num_seqs; b += 64) {
-            const int i = b + threadIdx.x;
-            seq += __popcll(__ballot(i < p.a.num_seqs && offset_of(p.a, i) <= row));
-        }
-        if (threadIdx.x == 0) seq_s = max(seq, 0);
+    int seq = -1;
+    for (int b = 0; b < p.a.num_seqs; b += 64) {
+        const int i = b + (threadIdx.x & 63);
+        seq += __popcll(__ballot(i < p.a.num_seqs && offset_of(p.a, i) <= row));
     }
-    __syncthreads();
-    const float c = rate_of(p.a.temperature[seq_s]);
+    const float c = rate_of(p.a.temperature[max(seq, 0)]);
     RowStat s{-INFINITY, 0.f, int(from), 0};
-    const int64_t base = row * V;
-    for (int64_t v = from + threadIdx.x * 4; v < to; v += kThreads * 4) {
-        float x[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        if (v + 4 <= to) {
-            load_four<BF16>(p.a.logits, base + v, x);
-        } else {
-            for (int j = 0; j < int(to - v); ++j) x[j] = load_one<BF16>(p.a.logits, base + v + j);
-        }
-        const float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+    auto add = [&](const float (&x)[8], int64_t v) {
+        float top = x[0];
+#pragma unroll
+        for (int j = 1; j < 8; ++j) top = fmaxf(top, x[j]);
         if (top > s.top) {
             s.sum *= s.top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((s.top - top) * c);
             s.top = top;
 #pragma unroll
-            for (int j = 3; j >= 0; --j)
+            for (int j = 7; j >= 0; --j)
                 if (x[j] == top) s.first = int(v) + j;
         }
         const float b = s.top == -INFINITY ? 0.f : s.top;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s.sum += __builtin_amdgcn_exp2f((x[j] - b) * c);
+        for (int j = 0; j < 8; ++j) s.sum += __builtin_amdgcn_exp2f((x[j] - b) * c);
+    };
+    while (v <= last) {
+        float y[kAhead][8];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[u][j] = x[u][j];
+        const int64_t next = v + kAhead * kMinRange;
+        if (next <= last) load(next);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) add(y[u], v + u * kMinRange);
+        v = next;
+    }
+    for (; v < to; v += kMinRange) {
+        float y[8];
+        if (v + kAtOnce <= to) load_eight<BF16>(p.a.logits, base + v, y);
+        else load_some<BF16>(p.a.logits, base + v, int(to - v), -INFINITY, y);
+        add(y, v);
     }
 #pragma unroll
     for (int m = 1; m < 64; m *= 2) s = join(s, shuffled(s, m), c);
@@ -152,24 +179,26 @@ struct Rest {
     float c, top, inv;
     int first;
     bool greedy;
-    const float* mass;
-    const int32_t* tokens;
+    const float* inv_mass;      // 1 / sum left before each tried child, in LDS
 
     __device__ float whole(float z, int64_t v) const {
         return greedy ? (v == first ? 1.f : 0.f) : __builtin_amdgcn_exp2f((z - top) * c) * inv;
     }
     __device__ float less(float r, float q, int tried) const {
-        for (int t = 0; t < tried; ++t) r = fmaxf(r / fmaxf(mass[t], 1e-30f) - q, 0.f);
+        for (int t = 0; t < tried; ++t) r = fmaxf(r * inv_mass[t] - q, 0.f);
         return r;
     }
 };
 
 template <bool Z16, bool Q16>
 __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(Params p) {
-    extern __shared__ int parents[];            // [max_nodes]
+    extern __shared__ int lds[];                // [3][max_nodes]
     __shared__ RowStat stat_s;
     __shared__ float sums[kWalkThreads / 64];
     const VerifyLaunch& a = p.a;
+    int* parents = lds;
+    int* tokens = lds + a.max_nodes;            // tried children's tokens
+    float* inv_mass = reinterpret_cast<float*>(lds + 2 * a.max_nodes);
     const int seq = blockIdx.x, lane = threadIdx.x & 63;
     const int first = offset_of(a, seq), n = min(max(0, offset_of(a, seq + 1) - first), a.max_nodes);
     int32_t* path = a.path + int64_t(seq) * a.max_nodes;
@@ -178,8 +207,6 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(Params p) {
         path[i] = -1;
     }
     const float temperature = a.temperature[seq], c = rate_of(temperature);
-    float* mass = p.mass + int64_t(seq) * a.max_nodes;
-    int32_t* tokens = p.tried + int64_t(seq) * a.max_nodes;
     int at = 0, depth = 0, tried = 0;
     __syncthreads();
     while (n > 0) {
@@ -187,16 +214,15 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(Params p) {
         ++depth;
         const int64_t row = first + at;
         if (threadIdx.x < 64) {                 // join the row's ranges
-            RowStat s{-INFINITY, 0.f, 0, 0};
+            RowStat s{-INFINITY, 0.f, 0x7fffffff, 0};
             if (lane < p.ranges) s = p.stats[row * p.ranges + lane];
-            else s.first = 0x7fffffff;
 #pragma unroll
             for (int m = 1; m < 64; m *= 2) s = join(s, shuffled(s, m), c);
             if (lane == 0) stat_s = s;
         }
         __syncthreads();
         const RowStat stat = stat_s;
-        Rest<Z16, Q16> rest{p, row * a.vocab, c, stat.top, 1.f / stat.sum, stat.first, !(temperature > 0.f), mass, tokens};
+        const Rest<Z16, Q16> rest{p, row * a.vocab, c, stat.top, 1.f / stat.sum, stat.first, !(temperature > 0.f), inv_mass};
         tried = 0;
         int accepted = -1, child = at;
         float left = 1.f;                       // sum of what is left
@@ -227,7 +253,7 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(Params p) {
                 }
                 __syncthreads();                // everybody has read the lists
                 if (threadIdx.x == 0) {
-                    mass[tried] = left;
+                    inv_mass[tried] = 1.f / fmaxf(left, 1e-30f);
                     tokens[tried] = int(x);
                 }
                 ++tried;
@@ -236,8 +262,29 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(Params p) {
                     left -= r;
                 } else if (following >= 0) {    // the next child is measured against the sum of what is left
                     float sum = 0.f;
-                    for (int64_t v = threadIdx.x; v < a.vocab; v += kWalkThreads)
-                        sum += rest.less(rest.whole(load_one<Z16>(a.logits, rest.base + v), v), load_one<Q16>(a.draft, rest.base + v), tried);
+                    auto add = [&](const float (&z)[8], const float (&d)[8], int64_t v) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) sum += rest.less(rest.whole(z[j], v + j), d[j], tried);
+                    };
+                    constexpr int kStride = kWalkThreads * kAtOnce, kAhead = 4;
+                    int64_t v = threadIdx.x * kAtOnce;
+                    for (; v + (kAhead - 1) * kStride + kAtOnce <= a.vocab; v += kAhead * kStride) {
+                        float z[kAhead][8], d[kAhead][8];
+#pragma unroll
+                        for (int u = 0; u < kAhead; ++u) {
+                            load_eight<Z16>(a.logits, rest.base + v + u * kStride, z[u]);
+                            load_eight<Q16>(a.draft, rest.base + v + u * kStride, d[u]);
+                        }
+#pragma unroll
+                        for (int u = 0; u < kAhead; ++u) add(z[u], d[u], v + u * kStride);
+                    }
+                    for (; v < a.vocab; v += kStride) {
+                        float z[8], d[8];
+                        const int some = int(min(int64_t(8), a.vocab - v));
+                        load_some<Z16>(a.logits, rest.base + v, some, -INFINITY, z);    // a weight of 0
+                        load_some<Q16>(a.draft, rest.base + v, some, 0.f, d);
+                        add(z, d, v);
+                    }
 #pragma unroll
                     for (int m = 1; m < 64; m *= 2) sum += __shfl_xor(sum, m);
                     if (lane == 0) sums[threadIdx.x / 64] = sum;
@@ -252,6 +299,10 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(Params p) {
         if (accepted < 0) break;
         at = accepted;
     }
+    for (int i = threadIdx.x; i < tried; i += kWalkThreads) {
+        p.mass[int64_t(seq) * a.max_nodes + i] = inv_mass[i];
+        p.tried[int64_t(seq) * a.max_nodes + i] = tokens[i];
+    }
     if (threadIdx.x == 0) {
         a.counts[seq] = depth;
         p.last[seq] = Last{n > 0 ? first + at : -1, tried, stat_s.top, stat_s.sum, stat_s.first, 0u};
@@ -261,80 +312,96 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(Params p) {
 
 template <bool Z16, bool Q16>
 __global__ __launch_bounds__(kThreads) void verify_sample_kernel(Params p) {
+    extern __shared__ int lds[];                // [2][max_nodes]
     __shared__ Best part[kThreads / 64];
-    __shared__ unsigned arrived;
     const VerifyLaunch& a = p.a;
-    const int seq = blockIdx.x / p.ranges, range = blockIdx.x - seq * p.ranges;
+    const int seq = blockIdx.x / p.sample_ranges, range = blockIdx.x - seq * p.sample_ranges;
     const Last last = p.last[seq];
     if (last.row < 0) return;
-    const float temperature = a.temperature[seq];
-    const float* mass = p.mass + int64_t(seq) * a.max_nodes;
-    const int32_t* tokens = p.tried + int64_t(seq) * a.max_nodes;
-    const Rest<Z16, Q16> rest{p, int64_t(last.row) * a.vocab, rate_of(temperature), last.top, 1.f / last.sum, last.first, !(temperature > 0.f), mass, tokens};
-    const float* noise = a.noise + int64_t(seq) * a.vocab;
-    const int64_t from = range * p.range, to = min(a.vocab, from + p.range);
-    Best b{0.f, 0.f, 0x7fffffff, 0x7fffffff};
-    for (int64_t v = from + threadIdx.x * 4; v < to; v += kThreads * 4) {
-        float z[4], q[4] = {0.f, 0.f, 0.f, 0.f}, e[4];
-        const int some = int(min(int64_t(4), to - v));
-        if (some == 4) {
-            load_four<Z16>(a.logits, rest.base + v, z);
-            load_four<false>(noise, v, e);
-            if (a.draft && last.tried) load_four<Q16>(a.draft, rest.base + v, q);
-        } else {
-            for (int j = 0; j < some; ++j) {
-                z[j] = load_one<Z16>(a.logits, rest.base + v + j);
-                e[j] = noise[v + j];
-                if (a.draft && last.tried) q[j] = load_one<Q16>(a.draft, rest.base + v + j);
-            }
+    float* inv_mass = reinterpret_cast<float*>(lds);
+    int* tokens = lds + a.max_nodes;
+    if (last.tried) {
+        for (int i = threadIdx.x; i < last.tried; i += kThreads) {
+            inv_mass[i] = p.mass[int64_t(seq) * a.max_nodes + i];
+            tokens[i] = p.tried[int64_t(seq) * a.max_nodes + i];
         }
-        for (int j = 0; j < some; ++j) {
+        __syncthreads();
+    }
+    const float temperature = a.temperature[seq];
+    const Rest<Z16, Q16> rest{p, int64_t(last.row) * a.vocab, rate_of(temperature), last.top, 1.f / last.sum, last.first, !(temperature > 0.f), inv_mass};
+    const float* noise = a.noise + int64_t(seq) * a.vocab;
+    const bool drafted = a.draft && last.tried;
+    const int64_t from = range * p.sample_range, to = min(a.vocab, from + p.sample_range);
+    Best b{0.f, 0x7fffffff, 0.f, 0x7fffffff};
+    for (int64_t v = from + threadIdx.x * kAtOnce; v < to; v += kMinRange) {
+        float z[8], q[8], e[8];
+        if (v + kAtOnce <= to) {
+            load_eight<Z16>(a.logits, rest.base + v, z);
+            load_eight<false>(noise, v, e);
+            if (drafted) load_eight<Q16>(a.draft, rest.base + v, q);
+        } else {
+            const int some = int(to - v);
+            load_some<Z16>(a.logits, rest.base + v, some, -INFINITY, z);
+            load_some<false>(noise, v, some, 1.f, e);
+            if (drafted) load_some<Q16>(a.draft, rest.base + v, some, 0.f, q);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
             const int64_t x = v + j;
             const float w = rest.whole(z[j], x);
-            if (w / e[j] > b.all) b.all = w / e[j], b.all_at = int(x);
-            float r = w;
-            if (a.draft) r = rest.less(w, q[j], last.tried);
-            if (r / e[j] > b.rest) {
-                if (!a.draft)
-                    for (int t = 0; t < last.tried; ++t)
-                        if (tokens[t] == x) r = 0.f;
-                if (r / e[j] > b.rest) b.rest = r / e[j], b.rest_at = int(x);
+            float r = drafted ? rest.less(w, q[j], last.tried) : w;
+            const float near = __builtin_amdgcn_rcpf(e[j]) * 1.00001f;      // the quotient itself where it may be the largest
+            if (w * near > b.all) take(b.all, b.all_at, w / e[j], int(x));
+            if (r * near > b.rest) {
+                if (!a.draft)                   // a certain draft: nothing is left of a token that was tried
+                    for (int t = 0; t < last.tried; ++t) r = tokens[t] == x ? 0.f : r;
+                if (r > 0.f) take(b.rest, b.rest_at, r / e[j], int(x));
             }
         }
     }
+    auto best_of_wave = [&]() {
 #pragma unroll
-    for (int m = 1; m < 64; m *= 2) {
-        take(b.rest, b.rest_at, __shfl_xor(b.rest, m), __shfl_xor(b.rest_at, m));
-        take(b.all, b.all_at, __shfl_xor(b.all, m), __shfl_xor(b.all_at, m));
-    }
+        for (int m = 1; m < 64; m *= 2) {
+            take(b.rest, b.rest_at, __shfl_xor(b.rest, m), __shfl_xor(b.rest_at, m));
+            take(b.all, b.all_at, __shfl_xor(b.all, m), __shfl_xor(b.all_at, m));
+        }
+    };
+    best_of_wave();
     if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = b;
     __syncthreads();
+    if (threadIdx.x >= 64) return;
+    // The last range to arrive finishes the sequence (walk left the count at 0).  Ranges run on different XCDs: their
+    // results are written through and read past the L2s, which a fence would write back whole.
+    unsigned long long* mine = reinterpret_cast<unsigned long long*>(p.best + int64_t(seq) * p.sample_ranges);
+    unsigned arrived = 0;
     if (threadIdx.x == 0) {
         for (int w = 1; w < kThreads / 64; ++w) {
             take(b.rest, b.rest_at, part[w].rest, part[w].rest_at);
             take(b.all, b.all_at, part[w].all, part[w].all_at);
         }
-        Best* mine = p.best + int64_t(seq) * p.ranges;
-        mine[range] = b;
-        // the last range to arrive finishes the sequence (walk left the count at 0)
-        __threadfence();
-        arrived = __hip_atomic_fetch_add(&p.last[seq].arrived, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
-        if (arrived == unsigned(p.ranges) - 1) {
-            __threadfence();
-            for (int i = 0; i < p.ranges; ++i) {
-                take(b.rest, b.rest_at, mine[i].rest, mine[i].rest_at);
-                take(b.all, b.all_at, mine[i].all, mine[i].all_at);
-            }
-            // nothing left (every probability went to the draft): the distribution itself; no finite logit: token 0
-            a.next[seq] = b.rest > 0.f ? b.rest_at : b.all > 0.f ? b.all_at : 0;
-        }
+        const u64x2 x = __builtin_bit_cast(u64x2, b);
+        __hip_atomic_store(mine + 2 * range, x[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(mine + 2 * range + 1, x[1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        arrived = __hip_atomic_fetch_add(&p.last[seq].arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
+    if (__shfl(arrived, 0) != unsigned(p.sample_ranges) - 1) return;
+    b = Best{0.f, 0x7fffffff, 0.f, 0x7fffffff};
+    if (threadIdx.x < unsigned(p.sample_ranges))
+        b = __builtin_bit_cast(Best, u64x2{__hip_atomic_load(mine + 2 * threadIdx.x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT),
+                                           __hip_atomic_load(mine + 2 * threadIdx.x + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)});
+    best_of_wave();
+    // nothing left (every probability went to the draft): the distribution itself; no finite logit: token 0
+    if (threadIdx.x == 0) a.next[seq] = b.rest > 0.f ? b.rest_at : b.all > 0.f ? b.all_at : 0;
 }
 
+// Ranges of a row: as many as give a few thousand workgroups, of at least one
+// load for every lane, and one lane to join each.
 int ranges_of(int64_t vocab, int64_t rows) {
     const int64_t most = (vocab + kMinRange - 1) / kMinRange;
     return int(std::max<int64_t>(1, std::min<int64_t>({most, kMaxRanges, (2048 + rows - 1) / std::max<int64_t>(rows, 1)})));
 }
+int64_t range_of(int64_t vocab, int ranges) { return ((vocab + ranges - 1) / ranges + kMinRange - 1) / kMinRange * kMinRange; }
 
 int64_t round16(int64_t x) { return (x + 15) & ~int64_t(15); }
 
@@ -345,29 +412,30 @@ hipError_t verify_as(const Params& p, hipStream_t stream) {
         hipLaunchKernelGGL((verify_stats_kernel<Z16>), dim3(uint32_t(a.total * p.ranges)), dim3(kThreads), 0, stream, p);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL((verify_walk_kernel<Z16, Q16>), dim3(a.num_seqs), dim3(kWalkThreads), a.max_nodes * sizeof(int), stream, p);
+    hipLaunchKernelGGL((verify_walk_kernel<Z16, Q16>), dim3(a.num_seqs), dim3(kWalkThreads), 3 * a.max_nodes * sizeof(int), stream, p);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    hipLaunchKernelGGL((verify_sample_kernel<Z16, Q16>), dim3(uint32_t(a.num_seqs) * p.ranges), dim3(kThreads), 0, stream, p);
+    hipLaunchKernelGGL((verify_sample_kernel<Z16, Q16>), dim3(uint32_t(a.num_seqs) * p.sample_ranges), dim3(kThreads), 2 * a.max_nodes * sizeof(int), stream, p);
     return hipGetLastError();
 }
 
 }  // namespace
 
 int64_t verify_workspace_bytes(int64_t vocab, int64_t total, int num_seqs, int max_nodes) {
-    const int64_t r = ranges_of(vocab, total);
-    return total * r * sizeof(RowStat) + num_seqs * (r * sizeof(Best) + round16(sizeof(Last)) + 2 * round16(max_nodes * 4));
+    return total * ranges_of(vocab, total) * sizeof(RowStat) + num_seqs * (ranges_of(vocab, num_seqs) * sizeof(Best) + round16(sizeof(Last)) + 2 * round16(max_nodes * 4));
 }
 
 hipError_t launch_verify(const VerifyLaunch& a, hipStream_t stream) {
     Params p{};
     p.a = a;
     p.ranges = ranges_of(a.vocab, a.total);
-    p.range = ((a.vocab + p.ranges - 1) / p.ranges + 7) / 8 * 8;
+    p.range = range_of(a.vocab, p.ranges);
+    p.sample_ranges = ranges_of(a.vocab, a.num_seqs);
+    p.sample_range = range_of(a.vocab, p.sample_ranges);
     uint8_t* at = static_cast<uint8_t*>(a.ws);
     p.stats = reinterpret_cast<RowStat*>(at);
     at += a.total * p.ranges * sizeof(RowStat);
     p.best = reinterpret_cast<Best*>(at);
-    at += int64_t(a.num_seqs) * p.ranges * sizeof(Best);
+    at += int64_t(a.num_seqs) * p.sample_ranges * sizeof(Best);
     p.last = reinterpret_cast<Last*>(at);
     at += a.num_seqs * round16(sizeof(Last));
     p.mass = reinterpret_cast<float*>(at);
