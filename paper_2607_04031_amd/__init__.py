@@ -248,10 +248,18 @@ def _ptr(x) -> int | None:
     raise TypeError(f"cannot pass {type(x)!r} as a device pointer")
 
 
+_raw_stream = None      # device index -> its current stream's handle
+
+
 def _stream(stream) -> int | None:
+    global _raw_stream
     if stream is None:
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        if _raw_stream is None:
+            # the handle without the Stream object around it, which takes 2.7 us of a call
+            _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+                (lambda device: torch.cuda.current_stream(device).cuda_stream)
+        return _raw_stream(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -524,19 +532,19 @@ def rope(positions, inv_freq, sections=None, interleaved=False) -> Rope:
 
 def _rows(x, heads, head_dim):
     """(address, elements between rows) of [n, heads * head_dim] or [n, heads, head_dim] rows, each without gaps."""
+    shape, stride, width = x.shape, x.stride(), heads * head_dim
     if not x.is_cuda:
         raise ValueError("libtl needs device tensors")
-    tail = x.shape[1:]
-    if x.dim() not in (2, 3) or tail.numel() != heads * head_dim or x.stride(-1) != 1 or \
-            (x.dim() == 3 and x.shape[1] > 1 and x.stride(1) != x.shape[2]):
-        raise ValueError(f"rows of {heads} x {head_dim} elements without gaps are needed, not {tuple(x.shape)}")
-    return x.data_ptr(), x.stride(0) if x.shape[0] > 1 else heads * head_dim
+    if not (len(shape) == 2 and shape[1] == width and stride[1] == 1) and \
+            not (len(shape) == 3 and shape[1] * shape[2] == width and stride[2] == 1 and (shape[1] == 1 or stride[1] == shape[2])):
+        raise ValueError(f"rows of {heads} x {head_dim} elements without gaps are needed, not {tuple(shape)}")
+    return x.data_ptr(), stride[0] if shape[0] > 1 else width
 
 
 def _int32(*tensors):
     import torch
     for x in tensors:
-        if x is not None and x.dtype not in (torch.int32, torch.uint32):
+        if x is not None and x.dtype is not torch.int32 and x.dtype is not torch.uint32:
             raise ValueError("indexes, offsets and masks are int32")
 
 
@@ -553,8 +561,9 @@ def kv_append(q, k, v, cache: KVCache, slots, rope=None, q_out=None, stream=None
     import torch
     some = q if q is not None else k
     n, D, H = some.shape[0], cache.head_dim, cache.kv_heads
-    heads = 0 if q is None else q.shape[1:].numel() // D
-    _int32(slots)
+    heads = 0 if q is None else q.shape[1] if q.dim() == 3 else q.shape[1] // D
+    if k is not None:
+        _int32(slots)
     for x in (q, k, v):
         if x is not None and (x.dtype != some.dtype or x.shape[0] != n):
             raise ValueError("queries, keys and values are rows of one type")
@@ -603,7 +612,7 @@ def attention(q, cache: KVCache, page_table, lens, q_offsets, max_q, max_len, sc
         raise ValueError("queries are bfloat16")
     _int32(page_table, lens, q_offsets, mask)
     total, B, D = q.shape[0], lens.numel(), cache.head_dim
-    heads = q.shape[1:].numel() // D
+    heads = q.shape[1] if q.dim() == 3 else q.shape[1] // D
     if page_table.shape[0] != B or q_offsets.numel() != B + 1 or (mask is not None and mask.shape[0] != total):
         raise ValueError("one row per sequence, one more offset, one mask row per query row")
     qp, ldq = _rows(q, heads, D)

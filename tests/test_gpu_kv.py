@@ -265,3 +265,71 @@ def test_streams_and_graph_replay():
             np.testing.assert_array_equal(got.cpu().double().numpy(), _serve.E4M3[code] * np.exp2(e.astype(np.float64))[..., None])
         assert torch.equal(q_out.cpu(), new[0])
         torch.zeros(1000, device="cuda").sum().item()
+
+
+@pytest.mark.parametrize("D,elem,bf16,H,page", [(128, 1, True, 2, 64), (64, 1, False, 3, 128), (128, 2, False, 1, 64), (64, 2, True, 5, 256)])
+@pytest.mark.parametrize("start", [0, 1, 38])
+def test_many_rows_at_once(D, elem, bf16, H, page, start):
+    """Rows enough for the kernels that take windows of tokens: slots that
+    follow one another from any start, jump inside a window, or lie outside."""
+    import torch
+    n, Hq = 700, 3
+    banner(f"kv append / read of {n} rows D={D} elem={elem} bf16={bf16} H={H} page={page} start={start}")
+    rng = np.random.default_rng(start + D)
+    q, k, v = _rows(rng, n, Hq, D, bf16), _rows(rng, n, H, D, bf16), _rows(rng, n, H, D, bf16)
+    pages = -(-(n + start + 200) // page) + 1
+    slots = start + np.arange(n)
+    slots[200:] += 50                                      # a jump
+    slots[330:340] = slots[330:340][::-1]
+    slots[400:403] = [-1, pages * page, -2 ** 31]
+    slots[699] = 2 ** 31 - 1                               # windows that run past the end of the cache
+    ref = _serve.Cache(pages, H, D, page, elem)
+    for i, s in enumerate(slots):
+        ref.put(s, k[i].double().numpy(), v[i].double().numpy())
+    cache = _serve.Cache(pages, H, D, page, elem).device()
+    out = tl.kv_append(q.cuda(), k.cuda(), v.cuda(), cache, _int(slots))
+    torch.cuda.synchronize()
+    assert torch.equal(out.cpu(), q.to(torch.bfloat16))
+    for got, want in zip(_serve.device_bytes(cache), ref.bytes()):
+        np.testing.assert_array_equal(got, want)
+    inside = (slots >= 0) & (slots < pages * page)
+    ko, vo = tl.kv_read(cache, _int(slots))
+    torch.cuda.synchronize()
+    for got, want in ((ko, ref.k), (vo, ref.v)):
+        got = got.cpu().double().numpy()
+        np.testing.assert_array_equal(got[inside], _serve.bf16(want[slots[inside]]))
+        assert not got[~inside].any()
+    only = torch.full((n, H, D), 7.0, dtype=torch.bfloat16, device="cuda")
+    tl.tl_kv_read(cache, _int(slots), n, None, only)
+    torch.cuda.synchronize()
+    assert torch.equal(only, vo)
+    # the last slots of the cache
+    tail = np.arange(pages * page - 600, pages * page)
+    tl.kv_append(None, k[:600].cuda(), v[:600].cuda(), cache, _int(tail))
+    ko, vo = tl.kv_read(cache, _int(tail))
+    torch.cuda.synchronize()
+    for i, s in enumerate(tail):
+        ref.put(s, k[i].double().numpy(), v[i].double().numpy())
+    np.testing.assert_array_equal(ko.cpu().double().numpy(), _serve.bf16(ref.k[tail]))
+    np.testing.assert_array_equal(vo.cpu().double().numpy(), _serve.bf16(ref.v[tail]))
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_many_rows_turn_as_few_rows_do(interleaved):
+    """The same rows at once and in pieces: the same bytes."""
+    import torch
+    n, Hq, H, D, page = 600, 5, 2, 128, 64
+    banner(f"kv append of {n} rows against pieces of 100, interleaved={interleaved}")
+    rng = np.random.default_rng(8)
+    q, k, v = (_rows(rng, n, h, D, True).cuda() for h in (Hq, H, H))
+    pos = _int(rng.integers(0, 5000, (3, n)))
+    freq = torch.from_numpy((10000.0 ** (-np.arange(48) / 48)).astype(np.float32)).cuda()
+    slots = _int(3 + np.arange(n))
+    one, many = (_serve.Cache(10, H, D, page, 1).device() for _ in range(2))
+    want = tl.kv_append(q, k, v, one, slots, tl.rope(pos, freq, (8, 16, 24), interleaved))
+    got = torch.cat([tl.kv_append(q[i:i + 100], k[i:i + 100], v[i:i + 100], many, slots[i:i + 100],
+                                  tl.rope(pos[:, i:i + 100].contiguous(), freq, (8, 16, 24), interleaved)) for i in range(0, n, 100)])
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+    for x, y in zip(_serve.device_bytes(one), _serve.device_bytes(many)):
+        np.testing.assert_array_equal(x, y)
