@@ -48,46 +48,21 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     const int heads = a.c.heads, group = a.q_heads / heads;
     const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
     const int wave = uniform(int(threadIdx.x >> 6)), key_wave = wave % kKeyWaves, row0 = wave / kKeyWaves * (16 * NT);
-    const int log2_chunks = a.c.log2_page - a.log2_keys;       // chunks of a page
-    Seq s;
-    int64_t place, place_end, total = 0;
-    int groups = a.groups, me = blockIdx.x;
-    AttnShared* shared = reinterpret_cast<AttnShared*>(a.ws + attn_shared_at<D>(a.groups, kRows));
-    if (a.split) {
-        attn_find(a, 0, &s, &total);
-        groups = attn_groups(a, total);
-        if (me < groups) me = attn_by_xcd(me, groups);
-        if (threadIdx.x == 0) shared[me].last = -1;
-        if (me >= groups) return;
-        place = me * total / groups;
-        place_end = (me + 1) * total / groups;
-    } else {
-        place = me;
-        place_end = me + 1;
-    }
-    const int64_t place0 = place;
+    __shared__ AttnLine line;
+    AttnRun run;
+    if (!attn_begin<D>(a, &line, &run)) return;
     for (int i = threadIdx.x; i < kRows * (D / 8); i += kThreads) odd_s[i] = 0;
     if (threadIdx.x == 0) odd_any = 0;
     __syncthreads();
-    while (place < place_end) {
-        if (!attn_find(a, place, &s, nullptr)) return;
-        // the piece: a tile's chunks [chunk0, chunk1)
-        const int64_t in_seq = place - s.before;
-        const int tile_of_seq = uniform(int(a.split ? in_seq / s.chunks : in_seq));
-        const int head = uniform(tile_of_seq / s.tiles), tile = tile_of_seq - head * s.tiles;
-        const int64_t tile_start = s.before + (a.split ? int64_t(tile_of_seq) * s.chunks : tile_of_seq);
-        const int chunk0 = uniform(a.split ? int(place - tile_start) : 0);
-        const int chunk1 = uniform(a.split ? int(min(int64_t(s.chunks), place_end - tile_start)) : s.chunks);
-        const bool whole = chunk0 == 0 && chunk1 == s.chunks;
-        const int64_t slot = 2 * int64_t(me) + (tile_start > place0 ? 1 : 0);
-        place = tile_start + (a.split ? chunk1 : 1);
-        if (a.split && tile_start >= place0 && chunk1 < s.chunks && threadIdx.x == 0)     // others go on with it
-            shared[me] = AttnShared{s.first, s.n, head, tile, attn_group_of(tile_start + s.chunks - 1, total, groups), int(slot)};
+    while (run.place < run.end) {
+        const AttnPiece piece = attn_piece<D>(a, &line, &run);
+        const Seq& s = piece.s;
+        const int head = piece.head, tile = piece.tile;
         // keys below 'all' are seen by every row of the wave, keys from 'end' on by none
         const int start = s.len - s.n, first_row = tile * kRows + row0;
         const int all = uniform(max(0, min(s.len, a.mask ? start : start + first_row / group + 1)));
         const int end = uniform(max(0, min(s.len, a.mask ? s.len : start + min(s.n - 1, (first_row + 16 * NT - 1) / group) + 1)));
-        const int chunk_end = first_row / group >= s.n ? 0 : min(chunk1, (end + kKeys - 1) / kKeys);
+        const int chunk_end = first_row / group >= s.n ? 0 : min(piece.chunk1, (end + kKeys - 1) / kKeys);
 
         // this lane's rows: queries as the second operand of K Q^T, in the order of the keys' chunks
         u32x4 q[kQueriesInLds ? 1 : NT][kQueriesInLds ? 1 : kSteps];
@@ -117,14 +92,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 #pragma unroll
             for (int db = 0; db < D / 16; ++db) o[nt][db] = f32x4v{0.f, 0.f, 0.f, 0.f};
         }
-        // a chunk's first key in the pool, in tokens; negative: a page that is none
-        const ConstInts table = ConstInts(a.page_table + int64_t(s.seq) * a.max_pages);
-        const int num_pages = int(a.c.num_pages), page_tokens = heads << a.c.log2_page, head_at = head << a.c.log2_page;
-        const int in_page = (1 << log2_chunks) - 1;
-        auto page_at = [&](int chunk) { return chunk < chunk_end ? table[chunk >> log2_chunks] : -1; };
-        auto block_of = [&](int chunk, int page) -> int64_t {
-            return page < 0 || page >= num_pages ? -1 : int64_t(page) * page_tokens + (head_at + (chunk & in_page) * kKeys);
-        };
+        const AttnPages pages(a, s.seq, head);
         // Keys of the next chunk are loaded under this one's softmax and second product, its values under the next one's
         // first, page numbers a chunk earlier.  Past the end (and for pages that are none) a block that exists is loaded.
         u32x4 kw[kBlocks][kPer], vw[kLoads], v_exp = {0, 0, 0, 0};
@@ -148,14 +116,15 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
             return u32x4{fp8_to_bf16<false>(w[2 * h], 1.f), fp8_to_bf16<true>(w[2 * h], 1.f),
                          fp8_to_bf16<false>(w[2 * h + 1], 1.f), fp8_to_bf16<true>(w[2 * h + 1], 1.f)};
         };
-        int chunk = chunk0 + key_wave;
-        int64_t block = block_of(chunk, page_at(chunk)), next = -1;
-        int next_page = page_at(chunk + kKeyWaves);
+        int chunk = piece.chunk0 + key_wave;
+        int64_t block = pages.block(chunk, pages.page(chunk, chunk_end)), next = -1;
+        int next_page = pages.page(chunk + kKeyWaves, chunk_end);
         uint32_t odd = 0;
         if (chunk < chunk_end) {
             load_keys(block);
             load_values(block);
         }
+        wait_for_loads();
         auto step = [&](auto is_masked) {
             constexpr bool masked = decltype(is_masked)::value;
             const int left = block < 0 ? 0 : s.len - chunk * kKeys - 4 * g;        // this lane's key 16 mb + i exists below that
@@ -224,10 +193,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
                     float top = -INFINITY;
 #pragma unroll
                     for (int e = 0; e < 4 * kB; ++e) top = fmaxf(top, x[nt][e >> 2][e & 3]);
-                    top = fmaxf(top, __shfl_xor(top, 16));
-                    top = fmaxf(top, __shfl_xor(top, 32));
-                    const float want = top * a.scale_log2;
-                    if (__ballot(want > m[nt] + kSlack)) {
+                    if (__ballot(top * a.scale_log2 > m[nt] + kSlack)) {
+                        top = fmaxf(top, __shfl_xor(top, 16));
+                        top = fmaxf(top, __shfl_xor(top, 32));
+                        const float want = top * a.scale_log2;
                         const float grown = fmaxf(m[nt], want);
                         const float shrink = __builtin_amdgcn_exp2f(m[nt] - (grown == -INFINITY ? 0.f : grown));
                         m[nt] = grown;
@@ -264,16 +233,16 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
             load_values(next);
         };
         // chunks that the wave's rows see whole, then the others
-        auto run = [&](auto is_masked, int before) {
+        auto go = [&](auto is_masked, int before) {
             for (; chunk < before; chunk += kKeyWaves) {
-                next = block_of(chunk + kKeyWaves, next_page);
-                next_page = page_at(chunk + 2 * kKeyWaves);
+                next = pages.block(chunk + kKeyWaves, next_page);
+                next_page = pages.page(chunk + 2 * kKeyWaves, chunk_end);
                 step(is_masked);
                 block = next;
             }
         };
-        run(std::false_type(), min(chunk_end, all / kKeys));
-        run(std::true_type(), chunk_end);
+        go(std::false_type(), min(chunk_end, all / kKeys));
+        go(std::true_type(), chunk_end);
 
         // join the waves that share rows
         if (__ballot(odd) && lane == 0) odd_any = 1;
@@ -307,73 +276,25 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
             __syncthreads();
         }
         if (odd_any) {
-            // infinities and NaNs among the values go in by themselves, one kind at a time, to the rows that see one
-            for (int c = chunk0 + key_wave; c < chunk_end; c += kKeyWaves) {
-                const int64_t at = block_of(c, page_at(c));
+            for (int c = piece.chunk0 + key_wave; c < chunk_end; c += kKeyWaves) {
+                const int64_t at = pages.block(c, pages.page(c, chunk_end));
                 if (c * kKeys + kKeys <= all || at < 0) continue;
-                const int left = s.len - c * kKeys - 4 * g;
 #pragma unroll 1
-                for (int nt = 0; nt < NT; ++nt) {
-                    const int row = row0 + nt * 16 + col, i = (tile * kRows + row) / group;
-                    const uint32_t seen = i < s.n ? attn_seen<kBlocks>(a, s, i, c * kKeys + 4 * g - start, left) : 0u;
-#pragma unroll 1
-                    for (int step = 0; step < 3 * (D / 16) * (kBlocks / 2); ++step) {
-                        const int kind = step % 3, db = step / 3 % (D / 16), h = step / 3 / (D / 16);
-                        u32x4 vf = reinterpret_cast<const u32x4*>(a.c.v + at * (D * ELEM))[db * 64 + lane], is, ones;
-                        if (ELEM == 1) {
-                            const uint32_t lo = h ? vf[2] : vf[0], hi = h ? vf[3] : vf[1];
-                            vf = u32x4{fp8_to_bf16<false>(lo, 1.f), fp8_to_bf16<true>(lo, 1.f), fp8_to_bf16<false>(hi, 1.f), fp8_to_bf16<true>(hi, 1.f)};
-                        }
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            vf[j] &= attn_first_halves(left - 32 * h - 16 * (j >> 1) - 2 * (j & 1));
-                            is[j] = attn_special(vf[j] & 0xffffu, kind) | attn_special(vf[j] >> 16, kind) << 16;
-                            const uint32_t two = seen >> (8 * h + 2 * j);
-                            ones[j] = (two & 1 ? 0x3f80u : 0u) | (two & 2 ? 0x3f800000u : 0u);
-                        }
-                        const f32x4v hits = mfma_16x16x32(is, ones, f32x4v{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)     // elements 16 db + 4 g + j of the row: 4 bits each
-                            if (hits[j] > 0.f) atomicOr(&odd_s[row * (D / 8) + db * 2 + (g >> 1)], 1u << (16 * (g & 1) + 4 * j + kind));
-                    }
-                }
+                for (int nt = 0; nt < NT; ++nt) attn_odd_chunk<D, ELEM, kBlocks>(a, piece, c, at, row0 + nt * 16 + col, odd_s);
             }
             __syncthreads();
         }
         for (int u = threadIdx.x; u < kRows * (D / 8); u += kThreads) {
             const int row = u / (D / 8), d = u % (D / 8) * 8;
-            const int at = tile * kRows + row, i = at / group;
-            if (i >= s.n) continue;
-            float top = m_s[0][row], sum = 0.f;
+            float top = m_s[0][row], sum = 0.f, x[8];
 #pragma unroll
             for (int w = 1; w < kKeyWaves; ++w) top = fmaxf(top, m_s[w][row]);
 #pragma unroll
             for (int w = 0; w < kKeyWaves; ++w) sum += l_s[w][row] * __builtin_amdgcn_exp2f(m_s[w][row] - (top == -INFINITY ? 0.f : top));
-            float* from = o_s + row * kPad + d;
-            if (odd_any) {
-                const uint32_t odd = odd_s[row * (D / 8) + d / 8];
-                for (int j = 0; j < 8; ++j) {
-                    if (odd >> (4 * j) & 1) from[j] += INFINITY;
-                    if (odd >> (4 * j) & 2) from[j] -= INFINITY;
-                    if (odd >> (4 * j) & 4) from[j] = NAN;
-                }
-            }
-            if (whole) {
-                const float inv = sum == 0.f ? 0.f : 1.f / sum;    // a row that sees no key: zeros
-                u32x4 w;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) w[j] = pack_bf16(from[2 * j] * inv, from[2 * j + 1] * inv);
-                *reinterpret_cast<u32x4*>(a.out + (int64_t(s.first + i) * a.q_heads + head * group + at - i * group) * D + d) = w;
-            } else {
-                float* part = a.ws + slot * attn_partial_floats<D>(kRows);
-#pragma unroll
-                for (int j = 0; j < 8; j += 4)
-                    *reinterpret_cast<f32x4v*>(part + row * D + d + j) = *reinterpret_cast<const f32x4v*>(from + j);
-                if (d == 0) {
-                    part[kRows * D + row] = top;
-                    part[kRows * D + kRows + row] = sum;
-                }
-            }
+            for (int j = 0; j < 8; ++j) x[j] = o_s[row * kPad + d + j];
+            if (odd_any) attn_add_odd(odd_s[row * (D / 8) + d / 8], x);
+            attn_put<D>(a, piece, row, d, x, top, sum);
         }
         __syncthreads();
         if (odd_any) {          // uniform
@@ -444,24 +365,20 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnLaunch a) {
 template <int D, int ELEM, int NT, int RG>
 hipError_t attn_as(const AttnLaunch& a, hipStream_t stream) {
     hipLaunchKernelGGL((attn_kernel<D, ELEM, NT, RG>), dim3(a.groups), dim3(kThreads), 0, stream, a);
-    hipError_t e = hipGetLastError();
-    if (e == hipSuccess && a.split) {
-        // few rows: their tiles are few too, with many parts each
-        if (a.rows <= 64) hipLaunchKernelGGL((attn_join_kernel<D, 4>), dim3(a.groups, a.rows / 4), dim3(kThreads), 0, stream, a);
-        else hipLaunchKernelGGL((attn_join_kernel<D, 16>), dim3(a.groups, a.rows / 16), dim3(kThreads), 0, stream, a);
-        e = hipGetLastError();
-    }
-    return e;
+    return hipGetLastError();
 }
 
 template <int D, int ELEM>
 hipError_t attn_rows(const AttnLaunch& a, hipStream_t stream) {
-    switch (a.rows) {
-        case 16: return attn_as<D, ELEM, 1, 1>(a, stream);
-        case 32: return attn_as<D, ELEM, 2, 1>(a, stream);
-        case 64: return attn_as<D, ELEM, 2, 2>(a, stream);
-        default: return attn_as<D, ELEM, 2, 4>(a, stream);
-    }
+    hipError_t e = a.rows == 16   ? attn_as<D, ELEM, 1, 1>(a, stream)
+                   : a.rows == 32 ? attn_as<D, ELEM, 2, 1>(a, stream)
+                   : a.rows == 64 ? attn_as<D, ELEM, 2, 2>(a, stream)
+                                  : launch_attn_wide(a, D, ELEM, stream);
+    if (e != hipSuccess || !a.split) return e;
+    // few rows: their tiles are few too, with many parts each
+    if (a.rows <= 64) hipLaunchKernelGGL((attn_join_kernel<D, 4>), dim3(a.groups, a.rows / 4), dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((attn_join_kernel<D, 16>), dim3(a.groups, a.rows / 16), dim3(kThreads), 0, stream, a);
+    return hipGetLastError();
 }
 
 }  // namespace

@@ -68,7 +68,7 @@ int64_t plan_attn(AttnLaunch* a, int head_dim, int elem_bytes) {
     constexpr int64_t kSlots = 2 * 256, kWholeKeys = 1024;
     const int64_t group = a->q_heads / a->c.heads, most = a->max_q * group;
     a->rows = most <= 16 ? 16 : most <= 32 ? 32 : most <= 64 ? 64 : 128;
-    a->log2_keys = elem_bytes == 1 ? 6 : 5;
+    a->log2_keys = elem_bytes == 1 || a->rows == 128 ? 6 : 5;
     a->max_tiles = std::min(a->num_seqs * ((most + a->rows - 1) / a->rows), a->total_q * group / a->rows + a->num_seqs) * a->c.heads;
     a->split = a->max_tiles < 4 * kSlots && a->max_len > kWholeKeys;
     a->groups = int(a->split ? kSlots : std::min<int64_t>(a->max_tiles, kMaxGrid));

@@ -104,6 +104,8 @@ struct AttnLaunch {
 // Fills the plan; returns the workspace it needs, in floats.
 int64_t plan_attn(AttnLaunch* a, int head_dim, int elem_bytes);
 hipError_t launch_attn(const AttnLaunch& a, int head_dim, int elem_bytes, hipStream_t stream);
+// its first launch where a.rows is 128
+hipError_t launch_attn_wide(const AttnLaunch& a, int head_dim, int elem_bytes, hipStream_t stream);
 
 struct VerifyLaunch {
     const void* logits;
