@@ -40,12 +40,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     constexpr int kPad = D + 4;
     // 32 rows over 8-bit keys: the queries stay in LDS (which holds the results later), for registers
     constexpr bool kQueriesInLds = NT == 2 && ELEM == 1 && D == 128;
-    __shared__ __attribute__((aligned(16))) float o_s[kRows * kPad];
+    __shared__ __attribute__((aligned(16))) float o_s[kWaves * 16 * NT * kPad];
     __shared__ float m_s[kKeyWaves][kRows], l_s[kKeyWaves][kRows];
     // rows' elements that an infinity (bit 0), -infinity (1) or NaN (2) among the values reaches: 4 bits each
     __shared__ uint32_t odd_s[kRows * (D / 8)];
     __shared__ int odd_any;
-    const int heads = a.c.heads, group = a.q_heads / heads;
     const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
     const int wave = uniform(int(threadIdx.x >> 6)), key_wave = wave % kKeyWaves, row0 = wave / kKeyWaves * (16 * NT);
     __shared__ AttnLine line;
@@ -60,9 +59,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
         const int head = piece.head, tile = piece.tile;
         // keys below 'all' are seen by every row of the wave, keys from 'end' on by none
         const int start = s.len - s.n, first_row = tile * kRows + row0;
-        const int all = uniform(max(0, min(s.len, a.mask ? start : start + first_row / group + 1)));
-        const int end = uniform(max(0, min(s.len, a.mask ? s.len : start + min(s.n - 1, (first_row + 16 * NT - 1) / group) + 1)));
-        const int chunk_end = first_row / group >= s.n ? 0 : min(piece.chunk1, (end + kKeys - 1) / kKeys);
+        const int all = uniform(max(0, min(s.len, a.mask ? start : start + attn_token(a, first_row) + 1)));
+        const int end = uniform(max(0, min(s.len, a.mask ? s.len : start + min(s.n - 1, attn_token(a, first_row + 16 * NT - 1)) + 1)));
+        const int chunk_end = attn_token(a, first_row) >= s.n ? 0 : min(piece.chunk1, (end + kKeys - 1) / kKeys);
 
         // this lane's rows: queries as the second operand of K Q^T, in the order of the keys' chunks
         u32x4 q[kQueriesInLds ? 1 : NT][kQueriesInLds ? 1 : kSteps];
@@ -71,9 +70,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const int row = first_row + nt * 16 + col;
-            own[nt] = row / group;
+            own[nt] = attn_token(a, row);
             const bool valid = own[nt] < s.n;
-            const uint16_t* qp = a.q + int64_t(s.first + (valid ? own[nt] : 0)) * a.ldq + int64_t(head * group + (valid ? row - own[nt] * group : 0)) * D;
+            const uint16_t* qp = a.q + int64_t(s.first + (valid ? own[nt] : 0)) * a.ldq + int64_t(head * a.group + (valid ? row - own[nt] * a.group : 0)) * D;
             if (!valid) own[nt] = -1;
 #pragma unroll
             for (int f = 0; f < kSteps; ++f) {
@@ -255,26 +254,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
                 l_s[key_wave][row0 + nt * 16 + col] = l[nt];
             }
         }
+        if (kQueriesInLds) __syncthreads();     // all have read their queries
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int db = 0; db < D / 16; ++db)
+                *reinterpret_cast<f32x4v*>(o_s + ((wave * NT + nt) * 16 + col) * kPad + db * 16 + 4 * g) = o[nt][db];
         __syncthreads();
-        for (int w = 0; w < kKeyWaves; ++w) {
-            if (key_wave == w) {
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const int row = row0 + nt * 16 + col;
-                    float top = m_s[0][row];
-#pragma unroll
-                    for (int i = 1; i < kKeyWaves; ++i) top = fmaxf(top, m_s[i][row]);
-                    const float f = __builtin_amdgcn_exp2f(m[nt] - (top == -INFINITY ? 0.f : top));
-#pragma unroll
-                    for (int db = 0; db < D / 16; ++db) {
-                        f32x4v* to = reinterpret_cast<f32x4v*>(o_s + row * kPad + db * 16 + 4 * g);
-                        // a wave without keys adds nothing (its m is -infinity: f and o are 0)
-                        *to = w ? *to + o[nt][db] * f : o[nt][db] * f;
-                    }
-                }
-            }
-            __syncthreads();
-        }
         if (odd_any) {
             for (int c = piece.chunk0 + key_wave; c < chunk_end; c += kKeyWaves) {
                 const int64_t at = pages.block(c, pages.page(c, chunk_end));
@@ -286,13 +272,20 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
         }
         for (int u = threadIdx.x; u < kRows * (D / 8); u += kThreads) {
             const int row = u / (D / 8), d = u % (D / 8) * 8;
-            float top = m_s[0][row], sum = 0.f, x[8];
+            // the waves that have the row, and its place with them
+            const int first = row / (16 * NT) * kKeyWaves, at = row % (16 * NT);
+            float top = m_s[0][row], sum = 0.f, x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int w = 1; w < kKeyWaves; ++w) top = fmaxf(top, m_s[w][row]);
 #pragma unroll
-            for (int w = 0; w < kKeyWaves; ++w) sum += l_s[w][row] * __builtin_amdgcn_exp2f(m_s[w][row] - (top == -INFINITY ? 0.f : top));
+            for (int w = 0; w < kKeyWaves; ++w) {
+                // a wave without keys adds nothing: its m is -infinity, its sums are 0
+                const float f = __builtin_amdgcn_exp2f(m_s[w][row] - (top == -INFINITY ? 0.f : top));
+                const float* from = o_s + ((first + w) * 16 * NT + at) * kPad + d;
+                sum += l_s[w][row] * f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = o_s[row * kPad + d + j];
+                for (int j = 0; j < 8; ++j) x[j] += from[j] * f;
+            }
             if (odd_any) attn_add_odd(odd_s[row * (D / 8) + d / 8], x);
             attn_put<D>(a, piece, row, d, x, top, sum);
         }
@@ -314,11 +307,11 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnLaunch a) {
     constexpr int kCols = D / 8, kParts = kThreads / (ROWS * kCols);
     __shared__ float o_s[kParts][ROWS][D];
     __shared__ float m_s[kParts][ROWS], l_s[kParts][ROWS];
-    const AttnShared t = reinterpret_cast<const AttnShared*>(a.ws + attn_shared_at<D>(a.groups, a.rows))[blockIdx.x];
-    const int group = a.q_heads / a.c.heads, floats = attn_partial_floats<D>(a.rows);
+    const AttnShared t = attn_shared<D>(a)[blockIdx.x];
+    const int rows = 1 << a.log2_rows, floats = attn_partial_floats<D>(rows);
     const int c = threadIdx.x % kCols * 8, j = threadIdx.x / kCols % ROWS, part = threadIdx.x / (kCols * ROWS);
-    const int row = blockIdx.y * ROWS + j, all_row = t.tile * a.rows + row, own = all_row / group;
-    if (t.last < 0 || (t.tile * a.rows + int(blockIdx.y) * ROWS) / group >= t.n) return;
+    const int row = blockIdx.y * ROWS + j, all_row = t.tile * rows + row, own = attn_token(a, all_row);
+    if (t.last < 0 || attn_token(a, t.tile * rows + int(blockIdx.y) * ROWS) >= t.n) return;
     float top = -INFINITY, sum = 0.f, o[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i] = 0.f;
@@ -326,7 +319,7 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnLaunch a) {
 #pragma unroll 4
         for (int w = blockIdx.x + part; w <= t.last; w += kParts) {
             const float* p = a.ws + (w == int(blockIdx.x) ? t.slot : 2 * int64_t(w)) * floats;
-            const float m = p[a.rows * D + row], l = p[a.rows * D + a.rows + row];
+            const float m = p[rows * D + row], l = p[rows * D + rows + row];
             const f32x4v lo = *reinterpret_cast<const f32x4v*>(p + row * D + c), hi = *reinterpret_cast<const f32x4v*>(p + row * D + c + 4);
             const float next = fmaxf(top, m), base = next == -INFINITY ? 0.f : next;
             const float f = __builtin_amdgcn_exp2f(top - base), h = __builtin_amdgcn_exp2f(m - base);
@@ -359,7 +352,7 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnLaunch a) {
     u32x4 w;
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = pack_bf16(o[2 * i] * inv, o[2 * i + 1] * inv);
-    *reinterpret_cast<u32x4*>(a.out + (int64_t(t.first + own) * a.q_heads + t.head * group + all_row - own * group) * D + c) = w;
+    *reinterpret_cast<u32x4*>(a.out + (int64_t(t.first + own) * a.q_heads + t.head * a.group + all_row - own * a.group) * D + c) = w;
 }
 
 template <int D, int ELEM, int NT, int RG>
@@ -370,14 +363,17 @@ hipError_t attn_as(const AttnLaunch& a, hipStream_t stream) {
 
 template <int D, int ELEM>
 hipError_t attn_rows(const AttnLaunch& a, hipStream_t stream) {
-    hipError_t e = a.rows == 16   ? attn_as<D, ELEM, 1, 1>(a, stream)
-                   : a.rows == 32 ? attn_as<D, ELEM, 2, 1>(a, stream)
-                   : a.rows == 64 ? attn_as<D, ELEM, 2, 2>(a, stream)
-                                  : launch_attn_wide(a, D, ELEM, stream);
+    hipError_t e = a.log2_rows == 4   ? attn_as<D, ELEM, 1, 1>(a, stream)
+                   : a.log2_rows == 5 ? attn_as<D, ELEM, 2, 1>(a, stream)
+                   : a.log2_rows == 6 ? attn_as<D, ELEM, 2, 2>(a, stream)
+                                      : launch_attn_wide(a, D, ELEM, stream);
     if (e != hipSuccess || !a.split) return e;
-    // few rows: their tiles are few too, with many parts each
-    if (a.rows <= 64) hipLaunchKernelGGL((attn_join_kernel<D, 4>), dim3(a.groups, a.rows / 4), dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((attn_join_kernel<D, 16>), dim3(a.groups, a.rows / 16), dim3(kThreads), 0, stream, a);
+    // the more parts a tile has, the more threads share a row's: with 170 parts (3 tiles of 64 rows) a row each is
+    // 8 us faster than four, with two parts (256 tiles of 16) 2.5 us slower
+    const int rows = 1 << a.log2_rows;
+    if (a.groups >= 32 * a.max_tiles && rows <= 64) hipLaunchKernelGGL((attn_join_kernel<D, 1>), dim3(a.groups, rows), dim3(kThreads), 0, stream, a);
+    else if (rows <= 64) hipLaunchKernelGGL((attn_join_kernel<D, 4>), dim3(a.groups, rows / 4), dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((attn_join_kernel<D, 16>), dim3(a.groups, rows / 16), dim3(kThreads), 0, stream, a);
     return hipGetLastError();
 }
 

@@ -33,6 +33,9 @@ struct Seq {
     int64_t before;             // places before the sequence
 };
 
+// the new token of a row: row / group
+__device__ inline int attn_token(const AttnLaunch& a, int row) { return int((__umulhi(uint32_t(row), a.group_magic) + uint32_t(row)) >> a.group_shift); }
+
 __device__ inline int attn_offset(const AttnLaunch& a, int i) { return max(0, min(a.q_offsets[i], int(a.total_q))); }
 
 // a value that all lanes of the wave have, in a scalar register
@@ -60,10 +63,9 @@ struct AttnLine {
 };
 
 __device__ inline void attn_sizes(const AttnLaunch& a, Seq* s) {
-    const int group = a.q_heads / a.c.heads;
-    s->tiles = int((int64_t(s->n) * group + a.rows - 1) / a.rows);
+    s->tiles = int((int64_t(s->n) * a.group + (1 << a.log2_rows) - 1) >> a.log2_rows);
     const bool rises = !a.mask && s->tiles > 1;
-    s->rise = rises ? ((a.rows << 4) / group) >> a.log2_keys : 0;
+    s->rise = rises ? attn_token(a, 16 << a.log2_rows) >> a.log2_keys : 0;
     s->cost = (((rises ? max(0, s->len - s->n) : s->len) + (1 << a.log2_keys) - 1) >> a.log2_keys) * 16 + kTileCost;
 }
 // places of the first t tiles of a head
@@ -180,7 +182,7 @@ struct AttnRun {
     int groups, me;
 };
 template <int D>
-__device__ inline AttnShared* attn_shared(const AttnLaunch& a) { return reinterpret_cast<AttnShared*>(a.ws + attn_shared_at<D>(a.groups, a.rows)); }
+__device__ inline AttnShared* attn_shared(const AttnLaunch& a) { return reinterpret_cast<AttnShared*>(a.ws + attn_shared_at<D>(a.groups, 1 << a.log2_rows)); }
 
 // false: the workgroup has nothing to do
 template <int D>
@@ -216,7 +218,6 @@ template <int D>
 __device__ inline AttnPiece attn_piece(const AttnLaunch& a, const AttnLine* line, AttnRun* r) {
     AttnPiece p;
     p.s = attn_find(a, line, r->place);
-    const int group = a.q_heads / a.c.heads;
     const int64_t in_seq = r->place - p.s.before;
     if (a.split) {
         const int64_t per_head = attn_cost(p.s, p.s.tiles);
@@ -227,7 +228,7 @@ __device__ inline AttnPiece attn_piece(const AttnLaunch& a, const AttnLine* line
         p.tile = p.s.tiles - 1 - uniform(int(in_seq - int64_t(p.head) * p.s.tiles));    // the longest first
     }
     // chunks that some row of the tile sees
-    const int last = min(p.s.n - 1, (p.tile * a.rows + a.rows - 1) / group);
+    const int last = min(p.s.n - 1, attn_token(a, ((p.tile + 1) << a.log2_rows) - 1));
     const int end = a.mask ? p.s.len : max(0, min(p.s.len, p.s.len - p.s.n + last + 1));
     const int chunks = (end + (1 << a.log2_keys) - 1) >> a.log2_keys;
     p.chunk0 = 0;
@@ -266,21 +267,21 @@ struct AttnPages {
 // Eight of a row's results, from d on: weighted sums o, their sum of weights l at the maximum m.
 template <int D>
 __device__ inline void attn_put(const AttnLaunch& a, const AttnPiece& p, int row, int d, const float (&o)[8], float m, float l) {
-    const int group = a.q_heads / a.c.heads, at = p.tile * a.rows + row, i = at / group;
+    const int rows = 1 << a.log2_rows, at = (p.tile << a.log2_rows) + row, i = attn_token(a, at);
     if (i >= p.s.n) return;
     if (p.whole) {
         const float inv = l == 0.f ? 0.f : 1.f / l;    // a row that sees no key: zeros
         u32x4 w;
 #pragma unroll
         for (int j = 0; j < 4; ++j) w[j] = pack_bf16(o[2 * j] * inv, o[2 * j + 1] * inv);
-        *reinterpret_cast<u32x4*>(a.out + (int64_t(p.s.first + i) * a.q_heads + p.head * group + at - i * group) * D + d) = w;
+        *reinterpret_cast<u32x4*>(a.out + (int64_t(p.s.first + i) * a.q_heads + p.head * a.group + at - i * a.group) * D + d) = w;
     } else {
-        float* part = a.ws + p.slot * attn_partial_floats<D>(a.rows);
+        float* part = a.ws + p.slot * attn_partial_floats<D>(rows);
 #pragma unroll
         for (int j = 0; j < 8; j += 4) *reinterpret_cast<f32x4v*>(part + row * D + d + j) = f32x4v{o[j], o[j + 1], o[j + 2], o[j + 3]};
         if (d == 0) {
-            part[a.rows * D + row] = m;
-            part[a.rows * D + a.rows + row] = l;
+            part[rows * D + row] = m;
+            part[rows * D + rows + row] = l;
         }
     }
 }
@@ -328,7 +329,7 @@ __device__ inline uint32_t attn_special(uint32_t x, int kind) {
 // (infinity, -infinity, NaN).
 template <int D, int ELEM, int MB>
 __device__ inline void attn_odd_chunk(const AttnLaunch& a, const AttnPiece& p, int c, int64_t block, int row, uint32_t* odd) {
-    const int lane = threadIdx.x & 63, g = lane >> 4, i = (p.tile * a.rows + row) / (a.q_heads / a.c.heads);
+    const int lane = threadIdx.x & 63, g = lane >> 4, i = attn_token(a, (p.tile << a.log2_rows) + row);
     const int key0 = c * (16 * MB) + 4 * g, left = p.s.len - key0;
     const uint32_t seen = i < p.s.n ? attn_seen<MB>(a, p.s, i, key0 - (p.s.len - p.s.n), left) : 0u;
 #pragma unroll 1

@@ -21,6 +21,24 @@ constexpr int kRows = 16 * kRowTiles * kWaves;
 constexpr int kKeys = 64;
 constexpr float kSlack = 8.f;
 
+// 16 bytes a lane from global memory (base + voff) to LDS, at the wave's base in the order of the lanes, past the
+// registers.  In assembly, since the compiler has every later read of LDS wait for such loads, also one of another buffer;
+// wait_for_loads() and a barrier stand before the reads that they are for.  Nothing else in the kernels uses M0.
+__device__ inline void load_to_lds(const uint8_t* base, uint32_t voff, u32x4* lds) {
+    const uint32_t la = uint32_t(uintptr_t((__attribute__((address_space(3))) void*)lds));
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(base), "s"(la) : "memory", "m0");
+#pragma clang diagnostic pop
+}
+
+// x, as a value that the compiler does not see through: what is computed of it is not computed ahead of loops, where
+// it would hold registers
+__device__ inline int hidden(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 template <int D, int ELEM>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void attn_wide_kernel(AttnLaunch a) {
     constexpr int kSteps = D / 32;                 // MFMA steps along the head
@@ -35,8 +53,6 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     static_assert(kWaves * 16 * kPad * 4 <= sizeof kv_s, "results of a row tile in the buffers");
     AttnRun run;
     if (!attn_begin<D>(a, &line, &run)) return;
-    const int group = a.q_heads / a.c.heads;
-    const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
     const int wave = uniform(int(threadIdx.x >> 6)), row0 = wave * (16 * kRowTiles);
     for (int i = threadIdx.x; i < kRows * (D / 8); i += kThreads) odd_s[i] = 0;
     if (threadIdx.x == 0) odd_any = 0;
@@ -44,11 +60,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     while (run.place < run.end) {
         const AttnPiece piece = attn_piece<D>(a, &line, &run);
         const Seq& s = piece.s;
+        const int thread = hidden(threadIdx.x), lane = thread & 63, g = lane >> 4, col = lane & 15;
         // keys below 'all' are seen by every row, keys from 'end' on by none: of the workgroup's, and of the wave's
         const int start = s.len - s.n;
-        auto all_of = [&](int first) { return max(0, min(s.len, a.mask ? start : start + first / group + 1)); };
+        auto all_of = [&](int first) { return max(0, min(s.len, a.mask ? start : start + attn_token(a, first) + 1)); };
         auto end_of = [&](int first, int count) {
-            return first / group >= s.n ? 0 : max(0, min(s.len, a.mask ? s.len : start + min(s.n - 1, (first + count - 1) / group) + 1));
+            return attn_token(a, first) >= s.n ? 0 : max(0, min(s.len, a.mask ? s.len : start + min(s.n - 1, attn_token(a, first + count - 1)) + 1));
         };
         const int first_row = piece.tile * kRows + row0;
         const int all_here = uniform(all_of(piece.tile * kRows)), all = uniform(all_of(first_row));
@@ -61,9 +78,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 #pragma unroll
         for (int nt = 0; nt < kRowTiles; ++nt) {
             const int row = first_row + nt * 16 + col;
-            own[nt] = row / group;
+            own[nt] = attn_token(a, row);
             const bool valid = own[nt] < s.n;
-            const uint16_t* qp = a.q + int64_t(s.first + (valid ? own[nt] : 0)) * a.ldq + int64_t(piece.head * group + (valid ? row - own[nt] * group : 0)) * D;
+            const uint16_t* qp = a.q + int64_t(s.first + (valid ? own[nt] : 0)) * a.ldq + int64_t(piece.head * a.group + (valid ? row - own[nt] * a.group : 0)) * D;
             if (!valid) own[nt] = -1;
 #pragma unroll
             for (int f = 0; f < kSteps; ++f) {
@@ -82,31 +99,50 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
         }
 
         const AttnPages pages(a, s.seq, piece.head);
-        u32x4 kw[kLoads], vw[kLoads];
+        u32x4 kw[ELEM == 1 ? kLoads : 1], vw[kLoads];
         uint32_t k_exp = 0, v_exp = 0, odd = 0;
-        auto fetch = [&](int64_t block) {       // for a page that is none: a block that exists
+        // the operand that load i of this wave's values is: (16 of the head's elements, 32 keys)
+        auto value_at = [&](int i) {
+            const int at = i * kWaves + wave;
+            return at % (D / 16) * 2 + at / (D / 16);
+        };
+        // A chunk from the pages (for a page that is none: from a block that exists): 16-bit entries straight into LDS, 8-bit
+        // ones into registers.
+        auto fetch = [&](int64_t block, int buffer) {
             const int64_t from = max(block, int64_t(0));
-            const u32x4* kp = reinterpret_cast<const u32x4*>(a.c.k + from * (D * ELEM)) + threadIdx.x;
-            const u32x4* vp = reinterpret_cast<const u32x4*>(a.c.v + from * (D * ELEM)) + threadIdx.x;
+            const uint8_t* kb = a.c.k + from * (D * ELEM);
+            const uint8_t* vb = a.c.v + from * (D * ELEM);
+            if (ELEM == 2) {
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) {
+                    const int at = i * kWaves + wave;
+                    load_to_lds(kb + at * 1024, lane * 16, kv_s[buffer][0] + at * 64);
+                    load_to_lds(vb + at * 1024, lane * 16, kv_s[buffer][1] + value_at(i) * 64);
+                }
+                return;
+            }
+            const u32x4* kp = reinterpret_cast<const u32x4*>(kb) + thread;
+            const u32x4* vp = reinterpret_cast<const u32x4*>(vb) + thread;
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) kw[i] = kp[i * kThreads];
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) vw[i] = vp[i * kThreads];
-            if (ELEM == 1) {
-                k_exp = *reinterpret_cast<const uint32_t*>(a.c.k_exp + from + col * 4);
-                if (threadIdx.x < kKeys) v_exp = a.c.v_exp[from + kv_value_exp_at(threadIdx.x)];
-            }
+            k_exp = *reinterpret_cast<const uint32_t*>(a.c.k_exp + from + col * 4);
+            if (thread < kKeys) v_exp = a.c.v_exp[from + kv_value_exp_at(thread)];
         };
-        auto put = [&](auto may_mask, int buffer, int chunk, int64_t block) {
+        // What is left to do to a chunk that was fetched: 8-bit entries become operands in LDS.  Where some row does not see
+        // all of it, entries past the end may be anything, and their scales and values count as 0; so do infinities and NaNs
+        // among the others for now: 0 * NaN would reach rows that do not see the key.
+        auto put = [&](auto may_mask, int buffer, int chunk) {
             u32x4* ks = kv_s[buffer][0] + lane;
             u32x4* vs = kv_s[buffer][1] + lane;
-            const int left = block < 0 ? 0 : s.len - chunk * kKeys;                 // keys of the chunk that exist
-            if (decltype(may_mask)::value && (chunk * kKeys + kKeys > all_here || block < 0)) {
-                // entries past the end may be anything: their scales and values count as 0.  So do infinities and NaNs
-                // among the others for now: 0 * NaN would reach rows that do not see the key
-                if (int(threadIdx.x) >= left) v_exp = 0;
+            const bool masked = decltype(may_mask)::value && chunk * kKeys + kKeys > all_here;
+            if (masked) {
+                const int left = s.len - chunk * kKeys;             // keys of the chunk that exist
+                if (thread >= left) v_exp = 0;
 #pragma unroll
-                for (int i = 0; i < kLoads; ++i)
+                for (int i = 0; i < kLoads; ++i) {
+                    if (ELEM == 2) vw[i] = vs[value_at(i) * 64];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const int first = ELEM == 1 ? 16 * j : (i * kWaves + wave) / (D / 16) * 32 + 16 * (j >> 1) + 2 * (j & 1);
@@ -115,33 +151,39 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
                         vw[i][j] &= ~bad;
                         odd |= bad;
                     }
+                    if (ELEM == 2) vs[value_at(i) * 64] = vw[i];
+                }
             }
+            if (ELEM == 2) return;
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 const int at = i * kWaves + wave;
-                if (ELEM == 1) {
-                    constexpr int kPer = D / 64;        // loads of a 16-key block
-                    const float scale = exp_scale(k_exp >> (8 * (at / kPer)) & 0xff);
+                constexpr int kPer = D / 64;            // loads of a 16-key block
+                const float scale = exp_scale(k_exp >> (8 * (at / kPer)) & 0xff);
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const uint32_t k0 = kw[i][2 * h], k1 = kw[i][2 * h + 1], v0 = vw[i][2 * h], v1 = vw[i][2 * h + 1];
-                        ks[(2 * at + h) * 64] = u32x4{fp8_to_bf16<false>(k0, scale), fp8_to_bf16<true>(k0, scale), fp8_to_bf16<false>(k1, scale), fp8_to_bf16<true>(k1, scale)};
-                        vs[(2 * at + h) * 64] = u32x4{fp8_to_bf16<false>(v0, 1.f), fp8_to_bf16<true>(v0, 1.f), fp8_to_bf16<false>(v1, 1.f), fp8_to_bf16<true>(v1, 1.f)};
-                    }
-                } else {
-                    ks[at * 64] = kw[i];
-                    vs[(at % (D / 16) * 2 + at / (D / 16)) * 64] = vw[i];
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t k0 = kw[ELEM == 1 ? i : 0][2 * h], k1 = kw[ELEM == 1 ? i : 0][2 * h + 1], v0 = vw[i][2 * h], v1 = vw[i][2 * h + 1];
+                    ks[(2 * at + h) * 64] = u32x4{fp8_to_bf16<false>(k0, scale), fp8_to_bf16<true>(k0, scale), fp8_to_bf16<false>(k1, scale), fp8_to_bf16<true>(k1, scale)};
+                    vs[(2 * at + h) * 64] = u32x4{fp8_to_bf16<false>(v0, 1.f), fp8_to_bf16<true>(v0, 1.f), fp8_to_bf16<false>(v1, 1.f), fp8_to_bf16<true>(v1, 1.f)};
                 }
             }
-            if (ELEM == 1 && threadIdx.x < kKeys) scale_s[buffer][threadIdx.x] = exp_scale(v_exp);
+            if (thread < kKeys) scale_s[buffer][thread] = exp_scale(v_exp);
         };
         // Operands are read from LDS four ahead of the products that take them: left to itself, the compiler reads one
         // and waits for it, twenty times a chunk.
-        auto compute = [&](auto may_mask, int buffer, int chunk, int64_t block) {
+        auto compute = [&](auto may_mask, int buffer, int chunk) {
             const u32x4* ks = kv_s[buffer][0] + lane;
             const u32x4* vs = kv_s[buffer][1] + lane;
+            // what the rows see, before the products need the registers
+            const bool masked = decltype(may_mask)::value && chunk * kKeys + kKeys > all;
+            uint32_t seen[kRowTiles];
+            if (masked) {
+                const int key0 = chunk * kKeys + 4 * g, left = s.len - key0;
+#pragma unroll
+                for (int nt = 0; nt < kRowTiles; ++nt) seen[nt] = own[nt] >= 0 ? attn_seen<4>(a, s, own[nt], key0 - start, left) : 0u;
+            }
             // S^T: keys 16 mb + 4 g + i of the chunk, row col
-            f32x4v x[kRowTiles][4], scale[4];
+            f32x4v x[kRowTiles][4];
             u32x4 kf[2][4], vf[2][4];
 #pragma unroll
             for (int nt = 0; nt < kRowTiles; ++nt)
@@ -158,10 +200,6 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
                 } else {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) vf[0][i] = vs[i * 64];
-                    if (ELEM == 1) {
-#pragma unroll
-                        for (int mb = 0; mb < 4; ++mb) scale[mb] = *reinterpret_cast<const f32x4v*>(&scale_s[buffer][16 * mb + 4 * g]);
-                    }
                 }
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -170,14 +208,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
                     for (int nt = 0; nt < kRowTiles; ++nt) x[nt][mb] = mfma_16x16x32(kf[f & 1][mb], q[nt][f], x[nt][mb]);
             }
             __builtin_amdgcn_sched_barrier(0);
-            if (decltype(may_mask)::value && (chunk * kKeys + kKeys > all || block < 0)) {
-                const int key0 = chunk * kKeys + 4 * g, left = block < 0 ? 0 : s.len - key0;
+            if (masked) {
 #pragma unroll
-                for (int nt = 0; nt < kRowTiles; ++nt) {
-                    const uint32_t seen = own[nt] >= 0 ? attn_seen<4>(a, s, own[nt], key0 - start, left) : 0u;
+                for (int nt = 0; nt < kRowTiles; ++nt)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) x[nt][e >> 2][e & 3] = seen >> e & 1 ? x[nt][e >> 2][e & 3] : -INFINITY;
-                }
+                    for (int e = 0; e < 16; ++e) x[nt][e >> 2][e & 3] = seen[nt] >> e & 1 ? x[nt][e >> 2][e & 3] : -INFINITY;
             }
             // running maximum and sum, as in attn_kernel
             u32x4 p[kRowTiles][2];
@@ -201,11 +236,16 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     float w[8];
+                    f32x4v scale[2];
+                    if (ELEM == 1) {
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) scale[b] = *reinterpret_cast<const f32x4v*>(&scale_s[buffer][16 * (2 * h + b) + 4 * g]);
+                    }
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(x[nt][2 * h + (e >> 2)][e & 3], a.scale_log2, -base));
                         l[nt] += y;
-                        w[e] = ELEM == 1 ? y * scale[2 * h + (e >> 2)][e & 3] : y;
+                        w[e] = ELEM == 1 ? y * scale[e >> 2][e & 3] : y;
                     }
                     p[nt][h] = u32x4{pack_bf16(w[0], w[1]), pack_bf16(w[2], w[3]), pack_bf16(w[4], w[5]), pack_bf16(w[6], w[7])};
                 }
@@ -227,28 +267,36 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
             __builtin_amdgcn_sched_barrier(0);
         };
 
-        // A chunk goes from the pages to registers during the one but one before it, and on into LDS at the start of the
-        // one before it.
+        // 8-bit chunks go from the pages to registers during the chunk but one before theirs, and on into LDS at the start of
+        // the one before; 16-bit ones into LDS during the one before.
+        constexpr int kAhead = ELEM == 1 ? 2 : 1;
         int64_t block = pages.block(piece.chunk0, pages.page(piece.chunk0, chunk_end));
         int64_t next = pages.block(piece.chunk0 + 1, pages.page(piece.chunk0 + 1, chunk_end));
         int next_page = pages.page(piece.chunk0 + 2, chunk_end);
         if (piece.chunk0 < chunk_end) {
-            fetch(block);
-            put(std::true_type(), 0, piece.chunk0, block);
-            fetch(next);
+            fetch(block, 0);
+            if (ELEM == 2) wait_for_loads();
+            put(std::true_type(), 0, piece.chunk0);
+            if (ELEM == 1) fetch(next, 0);
         }
         wait_for_loads();
         __syncthreads();
         // chunks that all rows see whole, and the next one too; then the others
         int chunk = piece.chunk0;
         auto go = [&](auto may_mask, int before) {
+            constexpr bool kMasked = decltype(may_mask)::value;
             for (; chunk < before; ++chunk) {
                 const int buffer = (chunk - piece.chunk0) & 1;
-                if (!decltype(may_mask)::value || chunk + 1 < chunk_end) put(may_mask, buffer ^ 1, chunk + 1, next);
+                const bool more = !kMasked || chunk + 1 < chunk_end;
+                if (ELEM == 1 && more) put(may_mask, buffer ^ 1, chunk + 1);
                 const int64_t after = pages.block(chunk + 2, next_page);
                 next_page = pages.page(chunk + 3, chunk_end);
-                fetch(after);
-                if (decltype(may_mask)::value ? chunk < wave_end : block >= 0) compute(may_mask, buffer, chunk, block);
+                if (ELEM == 1 || more) fetch(kAhead == 2 ? after : next, buffer ^ 1);
+                if (block >= 0 && (!kMasked || chunk < wave_end)) compute(may_mask, buffer, chunk);
+                if (ELEM == 2) {
+                    wait_for_loads();
+                    if (kMasked && more) put(may_mask, buffer ^ 1, chunk + 1);
+                }
                 block = next;
                 next = after;
                 __syncthreads();
@@ -257,7 +305,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
         go(std::false_type(), min(chunk_end, all_here / kKeys) - 1);
         go(std::true_type(), chunk_end);
 
-        if (__ballot(odd) && lane == 0) odd_any = 1;
+        if (__ballot(odd)) odd_any = 1;
         __syncthreads();
         if (odd_any) {
             for (int c = piece.chunk0; c < wave_end; ++c) {
@@ -267,6 +315,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
                 for (int nt = 0; nt < kRowTiles; ++nt) attn_odd_chunk<D, ELEM, 4>(a, piece, c, at, row0 + nt * 16 + col, odd_s);
             }
         }
+        const int lane2 = hidden(threadIdx.x & 63), g2 = lane2 >> 4, col2 = lane2 & 15;
         // a wave's results, a row tile at a time, through LDS of its own
         float* mine = reinterpret_cast<float*>(kv_s) + wave * 16 * kPad;
 #pragma unroll
@@ -274,9 +323,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
             l[nt] += __shfl_xor(l[nt], 16);
             l[nt] += __shfl_xor(l[nt], 32);
 #pragma unroll
-            for (int db = 0; db < D / 16; ++db) *reinterpret_cast<f32x4v*>(mine + col * kPad + db * 16 + 4 * g) = o[nt][db];
+            for (int db = 0; db < D / 16; ++db) *reinterpret_cast<f32x4v*>(mine + col2 * kPad + db * 16 + 4 * g2) = o[nt][db];
             __builtin_amdgcn_wave_barrier();
-            for (int u = lane; u < 16 * (D / 8); u += 64) {
+            for (int u = lane2; u < 16 * (D / 8); u += 64) {
                 const int r = u / (D / 8), row = row0 + nt * 16 + r, d = u % (D / 8) * 8;
                 float x[8];
 #pragma unroll

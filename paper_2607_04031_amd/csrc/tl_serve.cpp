@@ -66,13 +66,17 @@ int64_t span(int64_t rows, int64_t ld, int64_t width, int64_t elem) { return row
 // partial results costs a second launch.
 int64_t plan_attn(AttnLaunch* a, int head_dim, int elem_bytes) {
     constexpr int64_t kSlots = 2 * 256, kWholeKeys = 1024;
-    const int64_t group = a->q_heads / a->c.heads, most = a->max_q * group;
-    a->rows = most <= 16 ? 16 : most <= 32 ? 32 : most <= 64 ? 64 : 128;
-    a->log2_keys = elem_bytes == 1 || a->rows == 128 ? 6 : 5;
-    a->max_tiles = std::min(a->num_seqs * ((most + a->rows - 1) / a->rows), a->total_q * group / a->rows + a->num_seqs) * a->c.heads;
+    a->group = a->q_heads / a->c.heads;
+    a->group_shift = ilog2(a->group);
+    a->group_magic = uint32_t((uint64_t((int64_t(1) << a->group_shift) - a->group) << 32) / uint64_t(a->group) + 1);
+    const int64_t group = a->group, most = a->max_q * group;
+    a->log2_rows = most <= 16 ? 4 : most <= 32 ? 5 : most <= 64 ? 6 : 7;
+    const int64_t rows = int64_t(1) << a->log2_rows;
+    a->log2_keys = elem_bytes == 1 || rows == 128 ? 6 : 5;
+    a->max_tiles = std::min(a->num_seqs * ((most + rows - 1) / rows), a->total_q * group / rows + a->num_seqs) * a->c.heads;
     a->split = a->max_tiles < 4 * kSlots && a->max_len > kWholeKeys;
     a->groups = int(a->split ? kSlots : std::min<int64_t>(a->max_tiles, kMaxGrid));
-    return a->split ? 2 * a->groups * int64_t(a->rows) * (head_dim + 2) + a->groups * 8 : 0;
+    return a->split ? 2 * a->groups * rows * (head_dim + 2) + a->groups * 8 : 0;
 }
 
 }  // namespace tl

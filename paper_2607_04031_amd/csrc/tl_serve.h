@@ -92,10 +92,16 @@ struct AttnLaunch {
     int q_heads;
     float scale_log2;         // scale * log2(e)
     uint16_t* out;
-    // the plan: rows per tile, keys per chunk (a power of two), tiles of all
+    // query heads of a key head, and the division by it of x < 2^31 as
+    // (umulhi(x, magic) + x) >> shift (Granlund and Montgomery, "Division by
+    // invariant integers using multiplication", 1994, Section 4)
+    int group;
+    uint32_t group_magic;
+    int group_shift;
+    // the plan: rows per tile, keys per chunk (powers of two), tiles of all
     // sequences and heads (an upper bound), whether keys are split over
     // workgroups, and how many of those
-    int rows, log2_keys;
+    int log2_rows, log2_keys;
     bool split;
     int64_t max_tiles;
     int groups;
@@ -104,7 +110,7 @@ struct AttnLaunch {
 // Fills the plan; returns the workspace it needs, in floats.
 int64_t plan_attn(AttnLaunch* a, int head_dim, int elem_bytes);
 hipError_t launch_attn(const AttnLaunch& a, int head_dim, int elem_bytes, hipStream_t stream);
-// its first launch where a.rows is 128
+// its first launch where tiles have 128 rows
 hipError_t launch_attn_wide(const AttnLaunch& a, int head_dim, int elem_bytes, hipStream_t stream);
 
 struct VerifyLaunch {
