@@ -299,15 +299,40 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     }
 }
 
-// Joins the partial results of the tile that begins in workgroup blockIdx.x of
-// the first launch and ends in a later one, in their order: ROWS rows of it, a
-// thread for eight elements, the parts dealt to groups of threads.
-template <int D, int ROWS>
+// The workgroup of the first launch with the which-th of the tiles that it and
+// later ones share; -1: there are fewer.  Every wave finds it for itself.
+__device__ inline int attn_shared_tile(const AttnShared* notes, int groups, int which) {
+    const int lane = threadIdx.x & 63;
+    for (int base = 0; base < groups; base += 64 * 8) {
+        bool is[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int w = base + 64 * i + lane;
+            is[i] = notes[min(w, groups - 1)].last >= 0 && w < groups;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const unsigned long long some = __ballot(is[i]);
+            const unsigned long long it = __ballot(is[i] && __popcll(some & ((1ull << lane) - 1)) == which);
+            if (it) return base + 64 * i + __builtin_ctzll(it);
+            which -= __popcll(some);
+        }
+    }
+    return -1;
+}
+
+// Joins the partial results of a tile that begins in one workgroup of the first
+// launch and ends in a later one, in their order: ROWS rows of it, a thread for
+// eight elements, the parts dealt to groups of threads.  FEW tiles: the
+// blockIdx.x-th one that is shared; else the one of workgroup blockIdx.x.
+template <int D, int ROWS, bool FEW>
 __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnLaunch a) {
     constexpr int kCols = D / 8, kParts = kThreads / (ROWS * kCols);
     __shared__ float o_s[kParts][ROWS][D];
     __shared__ float m_s[kParts][ROWS], l_s[kParts][ROWS];
-    const AttnShared t = attn_shared<D>(a)[blockIdx.x];
+    const int begin = FEW ? uniform(attn_shared_tile(attn_shared<D>(a), a.groups, blockIdx.x)) : int(blockIdx.x);
+    if (begin < 0) return;
+    const AttnShared t = attn_shared<D>(a)[begin];
     const int rows = 1 << a.log2_rows, floats = attn_partial_floats<D>(rows);
     const int c = threadIdx.x % kCols * 8, j = threadIdx.x / kCols % ROWS, part = threadIdx.x / (kCols * ROWS);
     const int row = blockIdx.y * ROWS + j, all_row = t.tile * rows + row, own = attn_token(a, all_row);
@@ -317,8 +342,8 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnLaunch a) {
     for (int i = 0; i < 8; ++i) o[i] = 0.f;
     if (own < t.n) {
 #pragma unroll 4
-        for (int w = blockIdx.x + part; w <= t.last; w += kParts) {
-            const float* p = a.ws + (w == int(blockIdx.x) ? t.slot : 2 * int64_t(w)) * floats;
+        for (int w = begin + part; w <= t.last; w += kParts) {
+            const float* p = a.ws + (w == begin ? t.slot : 2 * int64_t(w)) * floats;
             const float m = p[rows * D + row], l = p[rows * D + rows + row];
             const f32x4v lo = *reinterpret_cast<const f32x4v*>(p + row * D + c), hi = *reinterpret_cast<const f32x4v*>(p + row * D + c + 4);
             const float next = fmaxf(top, m), base = next == -INFINITY ? 0.f : next;
@@ -371,9 +396,9 @@ hipError_t attn_rows(const AttnLaunch& a, hipStream_t stream) {
     // the more parts a tile has, the more threads share a row's: with 170 parts (3 tiles of 64 rows) a row each is
     // 8 us faster than four, with two parts (256 tiles of 16) 2.5 us slower
     const int rows = 1 << a.log2_rows;
-    if (a.groups >= 32 * a.max_tiles && rows <= 64) hipLaunchKernelGGL((attn_join_kernel<D, 1>), dim3(a.groups, rows), dim3(kThreads), 0, stream, a);
-    else if (rows <= 64) hipLaunchKernelGGL((attn_join_kernel<D, 4>), dim3(a.groups, rows / 4), dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((attn_join_kernel<D, 16>), dim3(a.groups, rows / 16), dim3(kThreads), 0, stream, a);
+    if (a.groups >= 32 * a.max_tiles && rows <= 64) hipLaunchKernelGGL((attn_join_kernel<D, 1, true>), dim3(a.max_tiles, rows), dim3(kThreads), 0, stream, a);
+    else if (rows <= 64) hipLaunchKernelGGL((attn_join_kernel<D, 4, false>), dim3(a.groups, rows / 4), dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((attn_join_kernel<D, 16, false>), dim3(a.groups, rows / 16), dim3(kThreads), 0, stream, a);
     return hipGetLastError();
 }
 
