@@ -35,6 +35,7 @@ import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libtl.so")
+CALLS_PATH = os.path.join(_HERE, "_tl_torch.so")
 
 TL_OK, TL_EINVAL, TL_EUNSUPPORTED, TL_EHIP, TL_ENOMEM, TL_ESCRATCH = 0, -1, -2, -3, -4, -5
 TL_NOALLOC_SCRATCH_BYTES = 64 << 20
@@ -147,9 +148,13 @@ class Rope:
     """tl_rope over tensors that it keeps alive."""
 
     def __init__(self, positions, inv_freq, sections, interleaved, rot_dim):
-        self.positions, self.inv_freq = positions, inv_freq
-        self.desc = RopeDesc(_ptr(positions), _ptr(inv_freq), rot_dim, len(sections),
-                             (ctypes.c_int32 * 3)(*(list(sections) + [0] * (3 - len(sections)))), int(interleaved))
+        self.positions, self.inv_freq, self.sections, self.interleaved = positions, inv_freq, sections, interleaved
+        self.rot_dim = rot_dim
+
+    @property
+    def desc(self) -> RopeDesc:
+        return RopeDesc(_ptr(self.positions), _ptr(self.inv_freq), self.rot_dim, len(self.sections),
+                        (ctypes.c_int32 * 3)(*(list(self.sections) + [0] * (3 - len(self.sections)))), int(self.interleaved))
 
 
 def _struct_dict(s):
@@ -278,6 +283,21 @@ def _desc(layout) -> LayoutDesc:
 def _check(rc: int, where: str):
     if rc != TL_OK:
         raise TLError(rc, where)
+
+
+_calls = None
+
+
+def _load_calls():
+    """The extension module that takes tensors to the serving-step entry points; its functions return a status, or None
+    for a call that needs the checks (or makes the outputs) below."""
+    global _calls
+    load_library()
+    if not os.path.exists(CALLS_PATH):
+        raise ImportError(f"_tl_torch.so is not built ({CALLS_PATH}); run python -m paper_2607_04031_amd.build")
+    from . import _tl_torch
+    _calls = _tl_torch
+    return _calls
 
 
 # ---------------------------------------------------------------------------
@@ -558,6 +578,9 @@ def _in_dtype(x):
 def kv_append(q, k, v, cache: KVCache, slots, rope=None, q_out=None, stream=None):
     """Rows of a QKV projection (tensors, or column ranges of one) into the cache at slots; returns the queries, turned by
     rope, as bf16 [n, q_heads, head_dim].  q may be None, and so may k and v."""
+    rc = (_calls or _load_calls()).kv_append(q, k, v, cache.desc, slots, rope, q_out, stream)
+    if rc is not None:
+        return q_out if rc == TL_OK else _check(rc, "tl_kv_append")
     import torch
     some = q if q is not None else k
     n, D, H = some.shape[0], cache.head_dim, cache.kv_heads
@@ -569,7 +592,7 @@ def kv_append(q, k, v, cache: KVCache, slots, rope=None, q_out=None, stream=None
             raise ValueError("queries, keys and values are rows of one type")
     if k is not None and slots.numel() != n:
         raise ValueError("one slot per row")
-    if rope is not None and rope.positions.numel() != n * rope.desc.axes:
+    if rope is not None and rope.positions.numel() != n * len(rope.sections):
         raise ValueError("one position per axis and row")
     (qp, ldq), (kp, ldk), (vp, ldv) = ((None, 0) if x is None else _rows(x, h, D) for x, h in ((q, heads), (k, H), (v, H)))
     if q is not None and q_out is None:
@@ -582,6 +605,9 @@ def kv_append(q, k, v, cache: KVCache, slots, rope=None, q_out=None, stream=None
 
 def kv_read(cache: KVCache, slots, k_out=None, v_out=None, stream=None):
     """bf16 keys and values [n, kv_heads, head_dim] of the given slots."""
+    rc = (_calls or _load_calls()).kv_read(cache.desc, slots, k_out, v_out, stream)
+    if rc is not None:
+        return (k_out, v_out) if rc == TL_OK else _check(rc, "tl_kv_read")
     import torch
     _int32(slots)
     n = slots.numel()
@@ -597,6 +623,9 @@ def kv_read(cache: KVCache, slots, k_out=None, v_out=None, stream=None):
 
 def kv_keep(cache: KVCache, page_table, starts, path, counts, stream=None):
     """Moves the entries of every sequence's accepted path (as verify returns it) to the front of its new tokens."""
+    rc = (_calls or _load_calls()).kv_keep(cache.desc, page_table, starts, path, counts, stream)
+    if rc is not None:
+        return _check(rc, "tl_kv_keep")
     _int32(page_table, starts, path, counts)
     B = page_table.shape[0]
     if starts.numel() != B or counts.numel() != B or path.shape[0] != B:
@@ -607,6 +636,10 @@ def kv_keep(cache: KVCache, page_table, starts, path, counts, stream=None):
 def attention(q, cache: KVCache, page_table, lens, q_offsets, max_q, max_len, scale, mask=None, out=None, stream=None):
     """Attention of the new tokens q [total_q, q_heads, head_dim] (bf16) over the cache: bf16 of q's shape.  mask: int32
     [total_q, words] of the new tokens that each new token sees, or None (causal)."""
+    rc = (_calls or _load_calls()).attention(q, cache.desc, page_table, lens, q_offsets, max_q, max_len, scale, mask, out,
+                                             stream)
+    if rc is not None:
+        return out if rc == TL_OK else _check(rc, "tl_attn")
     import torch
     if q.dtype != torch.bfloat16:
         raise ValueError("queries are bfloat16")
@@ -628,6 +661,11 @@ def attention(q, cache: KVCache, page_table, lens, q_offsets, max_q, max_len, sc
 def verify(logits, node_offsets, parents, tokens, temperature, uniform, noise, max_nodes, draft=None, out=None,
            stream=None):
     """(path int32 [sequences, max_nodes], counts, next): the drafted tokens that stay, and the token after them."""
+    path, count, after = out if out is not None else (None, None, None)
+    rc = (_calls or _load_calls()).verify(logits, node_offsets, parents, tokens, temperature, uniform, noise, max_nodes,
+                                          draft, path, count, after, stream)
+    if rc is not None:
+        return out if rc == TL_OK else _check(rc, "tl_verify")
     import torch
     _int32(node_offsets, parents, tokens)
     total, vocab = logits.shape

@@ -1,15 +1,18 @@
-"""Build libtl.so (HIP kernels + C ABI) in-tree for gfx950 with hipcc.
+"""Build libtl.so (HIP kernels + C ABI) in-tree for gfx950 with hipcc, and
+_tl_torch.so (host code that takes torch tensors to it) with the C++ compiler.
 
     python -m paper_2607_04031_amd.build          # or build() from Python
 """
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtl.so")
+CALLS = os.path.join(HERE, "_tl_torch.so")
 SOURCES = ["tl_api.cpp", "tl_read_amp.cpp", "tl_view.cpp", "tl_repack.hip", "tl_decode.hip", "tl_decode_fp8.hip",
            "tl_decode_lds.hip", "tl_lgms.hip", "tl_prefill.hip", "tl_view.hip", "tl_stream.hip",
            "tl_scratch.hip", "tl_decode_kn.hip", "tl_medium.hip", "tl_serve.cpp", "tl_kv.hip", "tl_attn.hip",
@@ -27,6 +30,19 @@ FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-I" + os.path.join(ROOT, "include"),
 ]
+
+
+def calls_command(out: str) -> list:
+    """Compiles the extension module over libtl; libtl is found beside it."""
+    import torch
+    home = os.path.dirname(torch.__file__)
+    rocm = os.path.dirname(os.path.dirname(HIPCC))
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__=1",
+            "-DUSE_ROCM=1", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+            "-isystem", os.path.join(home, "include"), "-isystem", os.path.join(rocm, "include"),
+            "-isystem", sysconfig.get_paths()["include"], os.path.join(CSRC, "tl_torch.cpp"), "-o", out,
+            "-L" + os.path.join(home, "lib"), "-ltorch_python", "-lc10_hip", "-lc10", "-ltorch_cpu",
+            "-L" + HERE, "-l:libtl.so", "-Wl,-rpath,$ORIGIN"]
 
 
 def build(verbose: bool = False, jobs: int = 8) -> str:
@@ -60,6 +76,10 @@ def build(verbose: bool = False, jobs: int = 8) -> str:
         print(" ".join(link), flush=True)
     subprocess.run(link, check=True)
     os.replace(LIB + ".tmp", LIB)
+    if verbose:
+        print(" ".join(calls_command(CALLS)), flush=True)
+    subprocess.run(calls_command(CALLS + ".tmp"), check=True)
+    os.replace(CALLS + ".tmp", CALLS)
     return LIB
 
 
