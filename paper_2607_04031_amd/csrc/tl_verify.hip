@@ -3,7 +3,10 @@
 //           and sum of exponentials -- all the bytes there are to read, so this
 //           is bound by HBM where the rows are many
 //   walk    a workgroup per sequence goes from the root to an accepted child
-//           while there is one
+//           while there is one.  Against a draft's distribution, each rejected
+//           child but a node's last costs a pass over the vocabulary, which one
+//           CU takes 13 us for at 131072 tokens (its vector units bound it), so
+//           that further workgroups of the sequence take parts of it
 //   sample  the last node's distribution less what its rejected children took,
 //           in ranges: the token with the largest ratio of weight to noise (an
 //           exponential race: P(token wins) is proportional to its weight)
@@ -22,6 +25,9 @@ constexpr int kWalkThreads = 1024;
 constexpr int kAtOnce = 8;                          // elements of a lane's load
 constexpr int kMinRange = kThreads * kAtOnce;       // one load of each lane
 constexpr int kMaxRanges = 64;                      // one lane joins each
+constexpr int kMaxParts = 64;                       // of a pass over the vocabulary in the walk; one lane joins each
+constexpr int kWalkers = 8;                         // workgroups of a sequence in the walk, at most
+constexpr int kMaxPolls = 1 << 16;                  // of a helper that waits for work
 constexpr float kLog2e = 1.44269504088896340736f;
 
 struct RowStat {
@@ -36,6 +42,19 @@ struct Last {           // what walk leaves for sample
     int first;
     unsigned arrived;
 };
+// What a walk's workgroups share.  The first one leads: it writes down a pass and opens its parts by 'claim'; whoever
+// adds to that takes a part, the leader too, and leaves its sum.  The leader waits for parts that were taken only, and a
+// helper for the leader no longer than kMaxPolls looks, so that no wait depends on which workgroups run at once.
+struct Pass {
+    int row, tried;     // a node's row; rejected children so far
+    float top, sum;
+    int first;
+    unsigned claim;     // pass << 8 | next part; kNoPart: none yet; kOver: the walk has ended
+    unsigned taken;     // parts done, of all passes
+    int pad;
+};
+constexpr unsigned kNoPart = 0x80, kOver = 0xffffff80u;   // their parts: past the last by far, and far from the byte's end
+static_assert(kMaxParts + 2 * kWalkers < 0x80, "a pass that everybody adds to once too often");
 struct Best {           // largest weight / noise of what is left, and of the whole distribution
     float rest;
     int rest_at;
@@ -49,11 +68,23 @@ struct Params {
     int ranges, sample_ranges;      // of a row, in stats and in sample
     int64_t range, sample_range;    // their elements, multiples of kMinRange
     RowStat* stats;     // [total][ranges]
+    int parts;          // of a pass over the vocabulary in the walk
+    int64_t part;       // their elements, a multiple of kWalkThreads * kAtOnce
+    int walkers;        // workgroups of a sequence in the walk
     Last* last;         // [num_seqs]
+    Pass* pass;         // [num_seqs]
+    float* sums;        // [num_seqs][kMaxParts]
     Best* best;         // [num_seqs][sample_ranges]
     float* mass;        // [num_seqs][max_nodes]: 1 / sum left before each tried child
     int32_t* tried;     // [num_seqs][max_nodes]: the tried children's tokens
 };
+
+template <typename T>
+__device__ inline void put_through(T* to, T x) { __hip_atomic_store(to, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+template <typename T>
+__device__ inline T read_past(const T* from) { return __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+// what was written through before is where others read it
+__device__ inline void wait_for_stores() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 __device__ inline int offset_of(const VerifyLaunch& a, int i) { return max(0, min(a.offsets[i], int(a.total))); }
 
@@ -106,6 +137,12 @@ __device__ inline RowStat shuffled(const RowStat& x, int m) {
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void verify_stats_kernel(Params p) {
     __shared__ RowStat part[kThreads / 64];
+    if (p.walkers > 1) {
+        for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < p.a.num_seqs; i += int64_t(gridDim.x) * kThreads) {
+            p.pass[i].claim = kNoPart;
+            p.pass[i].taken = 0;
+        }
+    }
     const int64_t row = blockIdx.x / p.ranges;
     const int range = blockIdx.x - int(row * p.ranges);
     const int64_t V = p.a.vocab, from = range * p.range, to = min(V, from + p.range);
@@ -190,39 +227,156 @@ struct Rest {
     }
 };
 
+// A thread's share of what is left of part 'part' of a node's distribution after 'tried' >= 1 rejected children.
+template <bool Z16, bool Q16>
+__device__ inline float left_of(const Params& p, const Rest<Z16, Q16>& rest, int tried, int part) {
+    const VerifyLaunch& a = p.a;
+    const int64_t to = min(a.vocab, (part + 1) * p.part);
+    const float scale = rest.inv_mass[0];
+    float sum = 0.f;
+    for (int64_t v = part * p.part + threadIdx.x * kAtOnce; v < to; v += kWalkThreads * kAtOnce) {
+        float z[8], d[8];
+        if (v + kAtOnce <= to) {
+            load_eight<Z16>(a.logits, rest.base + v, z);
+            load_eight<Q16>(a.draft, rest.base + v, d);
+        } else {
+            load_some<Z16>(a.logits, rest.base + v, int(to - v), -INFINITY, z);     // a weight of 0
+            load_some<Q16>(a.draft, rest.base + v, int(to - v), 0.f, d);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float r = fmaxf(rest.whole(z[j], v + j) * scale - d[j], 0.f);
+            for (int t = 1; t < tried; ++t) r = fmaxf(r * rest.inv_mass[t] - d[j], 0.f);
+            sum += r;
+        }
+    }
+    return sum;
+}
+
+// The sum over a workgroup, for its first wave.
+__device__ inline float sum_of(float x, float* waves) {
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) x += __shfl_xor(x, m);
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x / 64] = x;
+    __syncthreads();
+    x = (threadIdx.x & 63) < kWalkThreads / 64 ? waves[threadIdx.x & 63] : 0.f;
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) x += __shfl_xor(x, m);
+    return x;
+}
+
+// The walk's node and what was rejected of it: what a pass over the vocabulary has to know.
+struct Node {
+    int row, tried;
+    float top, sum;
+    int first;
+};
+
 template <bool Z16, bool Q16>
 __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(Params p) {
     extern __shared__ int lds[];                // [3][max_nodes]
-    __shared__ RowStat stat_s;
-    __shared__ float sums[kWalkThreads / 64];
+    constexpr int kHeld = 256;                  // nodes whose numbers are fetched ahead of the walk, all at once
+    __shared__ int token_s[kHeld];
+    __shared__ float uniform_s[kHeld], z_s[kHeld], q_s[kHeld];      // z, q: the token's, at its parent
+    __shared__ Node node_s;
+    __shared__ float waves[kWalkThreads / 64], sums_s[kMaxParts], left_s;
+    __shared__ int part_s, pass_s;
     const VerifyLaunch& a = p.a;
     int* parents = lds;
     int* tokens = lds + a.max_nodes;            // tried children's tokens
     float* inv_mass = reinterpret_cast<float*>(lds + 2 * a.max_nodes);
-    const int seq = blockIdx.x, lane = threadIdx.x & 63;
+    const int seq = blockIdx.x % a.num_seqs, lane = threadIdx.x & 63;
+    const bool leads = int(blockIdx.x) < a.num_seqs;    // the first workgroups of the launch, which start first
+    const float temperature = a.temperature[seq], c = rate_of(temperature);
+    Pass* shared = p.pass + seq;
+    float* mass = p.mass + int64_t(seq) * a.max_nodes;
+    float* sums = p.sums + int64_t(seq) * kMaxParts;
+    auto rest_of = [&](const Node& x) {
+        return Rest<Z16, Q16>{p, x.row * a.vocab, c, x.top, 1.f / x.sum, x.first, !(temperature > 0.f), inv_mass};
+    };
+    // Takes parts of passes while some are open; a helper reads what they are about.  Thread 0 alone looks at what the
+    // workgroups share.
+    auto take_parts = [&](int known) {
+        for (;;) {
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                const unsigned x = __hip_atomic_fetch_add(&shared->claim, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                part_s = (x & 0xff) < unsigned(p.parts) ? int(x & 0xff) : -1;
+                pass_s = int(x >> 8);
+            }
+            __syncthreads();
+            const int part = part_s;
+            if (part < 0) return known;
+            if (pass_s != known) {              // it stays as it is until this part is done
+                known = pass_s;
+                if (threadIdx.x == 0)
+                    node_s = Node{read_past(&shared->row), read_past(&shared->tried), read_past(&shared->top), read_past(&shared->sum), read_past(&shared->first)};
+                __syncthreads();
+                for (int i = threadIdx.x; i < node_s.tried; i += kWalkThreads) inv_mass[i] = read_past(mass + i);
+                __syncthreads();
+            }
+            const Node node = node_s;
+            const float sum = sum_of(left_of(p, rest_of(node), node.tried, part), waves);
+            if (threadIdx.x == 0) {
+                put_through(sums + part, sum);
+                wait_for_stores();
+                __hip_atomic_fetch_add(&shared->taken, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+        }
+    };
+    if (!leads) {
+        for (int known = 0;;) {
+            __syncthreads();                    // everybody has read part_s
+            if (threadIdx.x == 0) {
+                unsigned x = kNoPart;
+                for (int polls = 0; polls < kMaxPolls; ++polls) {
+                    x = read_past(&shared->claim);
+                    if (x >> 8 == kOver >> 8 || (x & 0xff) < unsigned(p.parts)) break;
+                    __builtin_amdgcn_s_sleep(4);
+                }
+                part_s = x >> 8 != kOver >> 8 && (x & 0xff) < unsigned(p.parts);
+            }
+            __syncthreads();
+            if (!part_s) return;
+            known = take_parts(known);
+        }
+    }
     const int first = offset_of(a, seq), n = min(max(0, offset_of(a, seq + 1) - first), a.max_nodes);
     int32_t* path = a.path + int64_t(seq) * a.max_nodes;
+    auto z_and_q = [&](int parent, int token, float* z, float* q) {
+        const int64_t at = (first + parent) * a.vocab + token;
+        *z = load_one<Z16>(a.logits, at);
+        *q = a.draft ? load_one<Q16>(a.draft, at) : 1.f;
+    };
     for (int i = threadIdx.x; i < a.max_nodes; i += kWalkThreads) {
-        if (i < n) parents[i] = a.parents[first + i];
+        if (i < n) {
+            const int parent = a.parents[first + i], token = a.tokens[first + i];
+            const float uniform = a.uniform[first + i];
+            parents[i] = parent;
+            if (i < kHeld) {
+                token_s[i] = token;
+                uniform_s[i] = uniform;
+                if (parent >= 0 && parent < i && token >= 0 && token < a.vocab) z_and_q(parent, token, z_s + i, q_s + i);
+            }
+        }
         path[i] = -1;
     }
-    const float temperature = a.temperature[seq], c = rate_of(temperature);
-    int at = 0, depth = 0, tried = 0;
+    int at = 0, depth = 0, tried = 0, passes = 0;
     __syncthreads();
     while (n > 0) {
         if (threadIdx.x == 0) path[depth] = at;
         ++depth;
-        const int64_t row = first + at;
+        const int row = first + at;
         if (threadIdx.x < 64) {                 // join the row's ranges
             RowStat s{-INFINITY, 0.f, 0x7fffffff, 0};
-            if (lane < p.ranges) s = p.stats[row * p.ranges + lane];
+            if (lane < p.ranges) s = p.stats[int64_t(row) * p.ranges + lane];
 #pragma unroll
             for (int m = 1; m < 64; m *= 2) s = join(s, shuffled(s, m), c);
-            if (lane == 0) stat_s = s;
+            if (lane == 0) node_s = Node{row, 0, s.top, s.sum, s.first};
         }
         __syncthreads();
-        const RowStat stat = stat_s;
-        const Rest<Z16, Q16> rest{p, row * a.vocab, c, stat.top, 1.f / stat.sum, stat.first, !(temperature > 0.f), inv_mass};
+        const Node node = node_s;
+        const Rest<Z16, Q16> rest = rest_of(node);
         tried = 0;
         int accepted = -1, child = at;
         float left = 1.f;                       // sum of what is left
@@ -235,62 +389,70 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(Params p) {
             return -1;
         };
         for (child = next_child(child); child >= 0;) {
-            const int64_t x = a.tokens[first + child];
+            const bool held = child < kHeld;
+            const int x = held ? token_s[child] : a.tokens[first + child];
             const int following = next_child(child);
             if (x >= 0 && x < a.vocab) {
-                float r = rest.whole(load_one<Z16>(a.logits, rest.base + x), x);
-                float q = 1.f;
+                float z, q;
+                if (held) z = z_s[child], q = q_s[child];
+                else z_and_q(at, x, &z, &q);
+                float r = rest.whole(z, x);
                 if (a.draft) {
-                    q = load_one<Q16>(a.draft, rest.base + x);
                     r = rest.less(r, q, tried);
                 } else {
                     for (int t = 0; t < tried; ++t)
                         if (tokens[t] == x) r = 0.f;
                 }
-                if (a.uniform[first + child] * q * left < r) {
+                if ((held ? uniform_s[child] : a.uniform[first + child]) * q * left < r) {
                     accepted = child;
                     break;
                 }
                 __syncthreads();                // everybody has read the lists
                 if (threadIdx.x == 0) {
                     inv_mass[tried] = 1.f / fmaxf(left, 1e-30f);
-                    tokens[tried] = int(x);
+                    tokens[tried] = x;
+                    node_s.tried = tried + 1;
+                    if (p.walkers > 1) put_through(mass + tried, inv_mass[tried]);
                 }
                 ++tried;
                 __syncthreads();
                 if (!a.draft) {
                     left -= r;
                 } else if (following >= 0) {    // the next child is measured against the sum of what is left
-                    float sum = 0.f;
-                    auto add = [&](const float (&z)[8], const float (&d)[8], int64_t v) {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) sum += rest.less(rest.whole(z[j], v + j), d[j], tried);
-                    };
-                    constexpr int kStride = kWalkThreads * kAtOnce, kAhead = 4;
-                    int64_t v = threadIdx.x * kAtOnce;
-                    for (; v + (kAhead - 1) * kStride + kAtOnce <= a.vocab; v += kAhead * kStride) {
-                        float z[kAhead][8], d[kAhead][8];
-#pragma unroll
-                        for (int u = 0; u < kAhead; ++u) {
-                            load_eight<Z16>(a.logits, rest.base + v + u * kStride, z[u]);
-                            load_eight<Q16>(a.draft, rest.base + v + u * kStride, d[u]);
+                    if (p.walkers > 1) {
+                        ++passes;
+                        if (threadIdx.x == 0) {
+                            put_through(&shared->row, node.row);
+                            put_through(&shared->tried, tried);
+                            put_through(&shared->top, node.top);
+                            put_through(&shared->sum, node.sum);
+                            put_through(&shared->first, node.first);
+                            wait_for_stores();
+                            put_through(&shared->claim, unsigned(passes) << 8);
+                            wait_for_stores();
                         }
-#pragma unroll
-                        for (int u = 0; u < kAhead; ++u) add(z[u], d[u], v + u * kStride);
+                        take_parts(passes);
+                        if (threadIdx.x == 0) {
+                            while (read_past(&shared->taken) < unsigned(passes * p.parts)) __builtin_amdgcn_s_sleep(1);
+                            asm volatile("" ::: "memory");
+                        }
+                        __syncthreads();
+                        if (lane < p.parts && threadIdx.x < 64) sums_s[lane] = read_past(sums + lane);
+                    } else {
+                        for (int part = 0; part < p.parts; ++part) {
+                            const float sum = sum_of(left_of(p, rest, tried, part), waves);
+                            if (threadIdx.x == 0) sums_s[part] = sum;
+                            __syncthreads();
+                        }
                     }
-                    for (; v < a.vocab; v += kStride) {
-                        float z[8], d[8];
-                        const int some = int(min(int64_t(8), a.vocab - v));
-                        load_some<Z16>(a.logits, rest.base + v, some, -INFINITY, z);    // a weight of 0
-                        load_some<Q16>(a.draft, rest.base + v, some, 0.f, d);
-                        add(z, d, v);
-                    }
+                    if (threadIdx.x < 64) {     // of all parts, in one order whoever took them
+                        float sum = lane < p.parts ? sums_s[lane] : 0.f;
 #pragma unroll
-                    for (int m = 1; m < 64; m *= 2) sum += __shfl_xor(sum, m);
-                    if (lane == 0) sums[threadIdx.x / 64] = sum;
+                        for (int m = 1; m < 64; m *= 2) sum += __shfl_xor(sum, m);
+                        if (lane == 0) left_s = sum;
+                    }
                     __syncthreads();
-                    left = 0.f;
-                    for (int w = 0; w < kWalkThreads / 64; ++w) left += sums[w];
+                    left = left_s;
                 }
             }
             child = following;
@@ -299,13 +461,14 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(Params p) {
         if (accepted < 0) break;
         at = accepted;
     }
+    if (p.walkers > 1 && threadIdx.x == 0) put_through(&shared->claim, kOver);
     for (int i = threadIdx.x; i < tried; i += kWalkThreads) {
-        p.mass[int64_t(seq) * a.max_nodes + i] = inv_mass[i];
+        mass[i] = inv_mass[i];
         p.tried[int64_t(seq) * a.max_nodes + i] = tokens[i];
     }
     if (threadIdx.x == 0) {
         a.counts[seq] = depth;
-        p.last[seq] = Last{n > 0 ? first + at : -1, tried, stat_s.top, stat_s.sum, stat_s.first, 0u};
+        p.last[seq] = Last{n > 0 ? first + at : -1, tried, node_s.top, node_s.sum, node_s.first, 0u};
         if (n == 0) a.next[seq] = -1;
     }
 }
@@ -380,16 +543,15 @@ __global__ __launch_bounds__(kThreads) void verify_sample_kernel(Params p) {
             take(b.all, b.all_at, part[w].all, part[w].all_at);
         }
         const u64x2 x = __builtin_bit_cast(u64x2, b);
-        __hip_atomic_store(mine + 2 * range, x[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        __hip_atomic_store(mine + 2 * range + 1, x[1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        put_through(mine + 2 * range, x[0]);
+        put_through(mine + 2 * range + 1, x[1]);
+        wait_for_stores();
         arrived = __hip_atomic_fetch_add(&p.last[seq].arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     if (__shfl(arrived, 0) != unsigned(p.sample_ranges) - 1) return;
     b = Best{0.f, 0x7fffffff, 0.f, 0x7fffffff};
     if (threadIdx.x < unsigned(p.sample_ranges))
-        b = __builtin_bit_cast(Best, u64x2{__hip_atomic_load(mine + 2 * threadIdx.x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT),
-                                           __hip_atomic_load(mine + 2 * threadIdx.x + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)});
+        b = __builtin_bit_cast(Best, u64x2{read_past(mine + 2 * threadIdx.x), read_past(mine + 2 * threadIdx.x + 1)});
     best_of_wave();
     // nothing left (every probability went to the draft): the distribution itself; no finite logit: token 0
     if (threadIdx.x == 0) a.next[seq] = b.rest > 0.f ? b.rest_at : b.all > 0.f ? b.all_at : 0;
@@ -412,7 +574,7 @@ hipError_t verify_as(const Params& p, hipStream_t stream) {
         hipLaunchKernelGGL((verify_stats_kernel<Z16>), dim3(uint32_t(a.total * p.ranges)), dim3(kThreads), 0, stream, p);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL((verify_walk_kernel<Z16, Q16>), dim3(a.num_seqs), dim3(kWalkThreads), 3 * a.max_nodes * sizeof(int), stream, p);
+    hipLaunchKernelGGL((verify_walk_kernel<Z16, Q16>), dim3(uint32_t(a.num_seqs) * p.walkers), dim3(kWalkThreads), 3 * a.max_nodes * sizeof(int), stream, p);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     hipLaunchKernelGGL((verify_sample_kernel<Z16, Q16>), dim3(uint32_t(a.num_seqs) * p.sample_ranges), dim3(kThreads), 2 * a.max_nodes * sizeof(int), stream, p);
     return hipGetLastError();
@@ -421,26 +583,36 @@ hipError_t verify_as(const Params& p, hipStream_t stream) {
 }  // namespace
 
 int64_t verify_workspace_bytes(int64_t vocab, int64_t total, int num_seqs, int max_nodes) {
-    return total * ranges_of(vocab, total) * sizeof(RowStat) + num_seqs * (ranges_of(vocab, num_seqs) * sizeof(Best) + round16(sizeof(Last)) + 2 * round16(max_nodes * 4));
+    return total * ranges_of(vocab, total) * sizeof(RowStat) +
+           num_seqs * (ranges_of(vocab, num_seqs) * sizeof(Best) + sizeof(Last) + sizeof(Pass) + kMaxParts * sizeof(float) + 2 * round16(max_nodes * 4));
 }
 
 hipError_t launch_verify(const VerifyLaunch& a, hipStream_t stream) {
+    constexpr int64_t kLoad = kWalkThreads * kAtOnce, kAtMost = 256;
     Params p{};
     p.a = a;
     p.ranges = ranges_of(a.vocab, a.total);
     p.range = range_of(a.vocab, p.ranges);
     p.sample_ranges = ranges_of(a.vocab, a.num_seqs);
     p.sample_range = range_of(a.vocab, p.sample_ranges);
+    // a part: one load for every lane; several workgroups to a sequence where it can reject two children against a draft,
+    // and no more than the CUs take at once
+    p.parts = int(std::min<int64_t>(kMaxParts, (a.vocab + kLoad - 1) / kLoad));
+    p.part = ((a.vocab + p.parts - 1) / p.parts + kLoad - 1) / kLoad * kLoad;
+    p.walkers = a.draft && a.max_nodes > 2 && a.total > 0 ? int(std::max<int64_t>(1, std::min<int64_t>({kWalkers, p.parts, kAtMost / a.num_seqs}))) : 1;
     uint8_t* at = static_cast<uint8_t*>(a.ws);
-    p.stats = reinterpret_cast<RowStat*>(at);
-    at += a.total * p.ranges * sizeof(RowStat);
-    p.best = reinterpret_cast<Best*>(at);
-    at += int64_t(a.num_seqs) * p.sample_ranges * sizeof(Best);
-    p.last = reinterpret_cast<Last*>(at);
-    at += a.num_seqs * round16(sizeof(Last));
-    p.mass = reinterpret_cast<float*>(at);
-    at += a.num_seqs * round16(a.max_nodes * 4);
-    p.tried = reinterpret_cast<int32_t*>(at);
+    auto take = [&](int64_t bytes) {
+        uint8_t* from = at;
+        at += bytes;
+        return from;
+    };
+    p.stats = reinterpret_cast<RowStat*>(take(a.total * p.ranges * sizeof(RowStat)));
+    p.best = reinterpret_cast<Best*>(take(int64_t(a.num_seqs) * p.sample_ranges * sizeof(Best)));
+    p.pass = reinterpret_cast<Pass*>(take(a.num_seqs * sizeof(Pass)));
+    p.sums = reinterpret_cast<float*>(take(a.num_seqs * kMaxParts * sizeof(float)));
+    p.mass = reinterpret_cast<float*>(take(a.num_seqs * round16(a.max_nodes * 4)));
+    p.tried = reinterpret_cast<int32_t*>(take(a.num_seqs * round16(a.max_nodes * 4)));
+    p.last = reinterpret_cast<Last*>(take(a.num_seqs * sizeof(Last)));
     if (a.logits_bf16) return a.draft_bf16 ? verify_as<true, true>(p, stream) : verify_as<true, false>(p, stream);
     return a.draft_bf16 ? verify_as<false, true>(p, stream) : verify_as<false, false>(p, stream);
 }
