@@ -399,9 +399,9 @@ hipError_t attn_rows(const AttnLaunch& a, hipStream_t stream) {
                                       : launch_attn_wide(a, D, ELEM, stream);
     if (e != hipSuccess || !a.split) return e;
     // the more parts a tile has, the more threads share a row's: with 170 parts (3 tiles of 64 rows) a row each is
-    // 8 us faster than four, with two parts (256 tiles of 16) 2.5 us slower
+    // 8 us faster than four, with 64 parts (8 tiles of 32) 3 us, with 42 (12 tiles of 16) 2.5 us slower
     const int rows = 1 << a.log2_rows;
-    if (a.groups >= 32 * a.max_tiles && rows <= 64) hipLaunchKernelGGL((attn_join_kernel<D, 1, true>), dim3(a.max_tiles, rows), dim3(kThreads), 0, stream, a);
+    if (a.groups >= 64 * a.max_tiles && rows <= 64) hipLaunchKernelGGL((attn_join_kernel<D, 1, true>), dim3(a.max_tiles, rows), dim3(kThreads), 0, stream, a);
     else if (rows <= 64) hipLaunchKernelGGL((attn_join_kernel<D, 4, false>), dim3(a.groups, rows / 4), dim3(kThreads), 0, stream, a);
     else hipLaunchKernelGGL((attn_join_kernel<D, 16, false>), dim3(a.groups, rows / 16), dim3(kThreads), 0, stream, a);
     return hipGetLastError();

@@ -151,10 +151,14 @@ __device__ inline Seq attn_find(const AttnLaunch& a, const AttnLine* line, int64
     return s;
 }
 
-// Workgroups that share T places: at least kMinCost of them each.
+// Workgroups that share T places: at least kMinCost of them each.  Where it
+// takes away few of them, a multiple of the tiles, so that tiles of one length
+// end where workgroups do: a second piece costs a workgroup 4 us.
 constexpr int kMinCost = 4 * 16 + kTileCost;
 __device__ inline int attn_groups(const AttnLaunch& a, int64_t total) {
-    return int(max(int64_t(1), min(int64_t(a.groups), (total + kMinCost - 1) / kMinCost)));
+    const int most = int(max(int64_t(1), min(int64_t(a.groups), (total + kMinCost - 1) / kMinCost)));
+    const int tiles = int(min(a.max_tiles, int64_t(most))), even = most / tiles * tiles;
+    return even >= most - most / 8 || (a.num_seqs == 1 && most >= 4 * tiles) ? even : most;
 }
 __device__ inline int attn_group_of(int64_t p, int64_t total, int groups) { return int(quotient((p + 1) * groups - 1, total)); }
 

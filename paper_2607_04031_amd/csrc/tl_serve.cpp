@@ -62,10 +62,19 @@ int64_t span(int64_t rows, int64_t ld, int64_t width, int64_t elem) { return row
 
 // Rows per tile: the fewest of 16, 32, 64 and 128 that hold a sequence's rows
 // of one key head.  Keys are split where the tiles are too few to keep the CUs
-// evenly busy, unless no sequence has more than kWholeKeys keys: joining the
-// partial results costs a second launch.
+// evenly busy, but not (us split and not, ragged lengths up to the one named):
+//   - where no sequence has more than 1024 keys (16 rows: 2048 of 8 bits, 1536 of
+//     16), since joining the partial results costs a second launch: one token
+//     over 2048 8-bit tokens 17.4 and 14.3 (over 3000 15.3 and 19.8), over 1500
+//     16-bit ones 16.2 and 14.8 (2048: 13.1 and 20.2);
+//   - where each of the slots for workgroups gets a tile of its own and none is
+//     long: 64 tokens over 2048 or 4096 39.0 and 33.7, 62.0 and 57.8; at 128 rows
+//     two tiles to a slot, which trees need (64 of 32 nodes over 2048 tokens 128
+//     and 121, 16-bit 135 and 117), and prompts, whose tiles differ, do not (8 of
+//     512 tokens 148 and 167);
+//   - where each gets four tiles.
 int64_t plan_attn(AttnLaunch* a, int head_dim, int elem_bytes) {
-    constexpr int64_t kSlots = 2 * 256, kWholeKeys = 1024;
+    constexpr int64_t kSlots = 2 * 256;
     a->group = a->q_heads / a->c.heads;
     a->group_shift = ilog2(a->group);
     a->group_magic = uint32_t((uint64_t((int64_t(1) << a->group_shift) - a->group) << 32) / uint64_t(a->group) + 1);
@@ -74,7 +83,10 @@ int64_t plan_attn(AttnLaunch* a, int head_dim, int elem_bytes) {
     const int64_t rows = int64_t(1) << a->log2_rows;
     a->log2_keys = elem_bytes == 1 || rows == 128 ? 6 : 5;
     a->max_tiles = std::min(a->num_seqs * ((most + rows - 1) / rows), a->total_q * group / rows + a->num_seqs) * a->c.heads;
-    a->split = a->max_tiles < 4 * kSlots && a->max_len > kWholeKeys;
+    const bool wide = rows == 128;
+    const int64_t whole = rows > 16 ? 1024 : elem_bytes == 1 ? 2048 : 1536;
+    const bool enough = wide ? a->mask && a->max_tiles >= 2 * kSlots && a->max_len <= 2048 : a->max_tiles >= kSlots && a->max_len <= 4096;
+    a->split = a->max_len > whole && !enough && a->max_tiles < 4 * kSlots;
     a->groups = int(a->split ? kSlots : std::min<int64_t>(a->max_tiles, kMaxGrid));
     return a->split ? 2 * a->groups * rows * (head_dim + 2) + a->groups * 8 : 0;
 }
