@@ -64,3 +64,15 @@ def test_repeats_are_equal_and_graphs_replay():
             assert all(torch.equal(x.cpu(), y) for x, y in zip(out, want))
         else:
             assert bool((out[1] >= 2).any())    # a uniform number of 0 accepts what has any weight
+
+
+@pytest.mark.parametrize("draft,bf16", [(None, False), ("f32", True), ("bf16", False)])
+def test_more_nodes_than_are_held(draft, bf16):
+    """Paths past node 256, whose numbers are read as the walk comes to them: every token accepted, then some rejected."""
+    banner(f"verify long paths draft={draft} bf16={bf16}")
+    c, bf16, draft = base._case(31, [400, 5, 290], 97, 1, draft, bf16)
+    c["uniform"][:] = 0.0
+    counts = base._check(c, bf16, draft)
+    c["uniform"][c["offsets"][0] + 300:c["offsets"][1]] = 0.97
+    fewer = base._check(c, bf16, draft)
+    assert counts[0] == 400 and 300 <= fewer[0] < 400
