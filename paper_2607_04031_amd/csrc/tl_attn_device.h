@@ -151,14 +151,16 @@ __device__ inline Seq attn_find(const AttnLaunch& a, const AttnLine* line, int64
     return s;
 }
 
-// Workgroups that share T places: at least kMinCost of them each.  Where it
-// takes away few of them, a multiple of the tiles, so that tiles of one length
-// end where workgroups do: a second piece costs a workgroup 4 us.
-constexpr int kMinCost = 4 * 16 + kTileCost;
+// Workgroups that share T places: at least kMinCost of them each (one token of
+// 64 heads over 8 and 8192 8-bit keys: 15.0 us; with 4 * 16 or 8 * 16 of chunks
+// 15.9 and 16.8).  Where it takes away few of them, or of one sequence, a
+// multiple of the tiles, so that tiles of one length end where workgroups do: a
+// second piece costs a workgroup 4 us (three tokens over 1100: 16.9 and 22.5).
+constexpr int kMinCost = 2 * 16 + kTileCost;
 __device__ inline int attn_groups(const AttnLaunch& a, int64_t total) {
     const int most = int(max(int64_t(1), min(int64_t(a.groups), (total + kMinCost - 1) / kMinCost)));
     const int tiles = int(min(a.max_tiles, int64_t(most))), even = most / tiles * tiles;
-    return even >= most - most / 8 || (a.num_seqs == 1 && most >= 4 * tiles) ? even : most;
+    return even >= most - most / 8 || (a.num_seqs == 1 && most >= 2 * tiles) ? even : most;
 }
 __device__ inline int attn_group_of(int64_t p, int64_t total, int groups) { return int(quotient((p + 1) * groups - 1, total)); }
 
