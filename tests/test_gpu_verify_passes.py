@@ -9,7 +9,7 @@ from tests._gpu import banner
 pytestmark = pytest.mark.gpu
 _lib = base._lib
 
-# seed, sizes, vocabulary, siblings: 8 workgroups to a sequence, 6, 3, and one
+# seed, sizes, vocabulary, siblings: 16 workgroups to a sequence, 5, 3, 3 and one
 CASES = {"one_sequence": (3, [24], 131072, 6), "parts_that_end_short": (1, [40, 1, 9], 40001, 4),
          "forty": (1, [5] * 40, 17000, 3), "eighty": (11, [4, 1, 3, 0] * 20, 24576, 3), "many": (2, [4] * 260, 9001, 3)}
 
