@@ -28,9 +28,9 @@
  *    inside a kernel surfaces at the caller's next synchronisation.
  *  - Calls are thread-safe.  The library owns, per (device, stream), a split-K
  *    workspace, a fetch counter and arrival counters (by which a small
- *    weight's K splits find out that all of them are done); concurrent calls on
- *    the SAME stream from several host threads are serialised by the stream, as
- *    usual.  A
+ *    weight's K splits find out that all of them are done); of concurrent calls
+ *    on the SAME stream from several host threads, one enqueues all that it has
+ *    to before the next one does (tl_gemm_noalloc aside, see there).  A
  *    workspace that must grow is replaced by a larger one and the old one is
  *    kept (not freed) until tl_release, so work already enqueued or captured
  *    with it stays valid.

@@ -45,8 +45,13 @@ namespace {
 // took the old pointer, may still use it.  Retired workspaces are freed by
 // tl_release.  Each call holds a shared reference to its state, so the
 // buffers it enqueues on outlive a concurrent tl_release's host-side cleanup.
+// A call's launches hand one another partial results in the workspace, and the
+// sets of counters alternate in the order of the launches: a call has its
+// state's 'enqueue' from the lookup until its last launch is enqueued, so that
+// no other host thread's call on the stream comes between.
 // ---------------------------------------------------------------------------
 struct StreamState {
+    std::mutex enqueue;
     int dev = 0;
     float* ws = nullptr;
     size_t ws_bytes = 0;
@@ -65,9 +70,11 @@ struct StreamState {
     }
 };
 
-// What one call uses: the buffers as they were when it looked them up.
+// What one call uses: the buffers as they were when it looked them up, and the
+// right to enqueue on them (given back before the state may go).
 struct StateRef {
     std::shared_ptr<StreamState> keep;
+    std::unique_lock<std::mutex> enqueue;
     float* ws = nullptr;
     unsigned long long* fetch = nullptr;
 
@@ -95,17 +102,22 @@ bool capturing(hipStream_t stream) {
 
 // Looks up (current device, stream), creating its tally and counters (cleared
 // on 'stream', so the clear is ordered before any kernel that uses it) and growing its
-// workspace to at least ws_bytes.  The lock covers the map and the
-// allocations only; nothing here waits for the GPU.
+// workspace to at least ws_bytes; *out has the state to itself until it goes.
+// The global lock covers the map only; nothing here waits for the GPU.
 int get_state(hipStream_t stream, size_t ws_bytes, StateRef* out) {
     int dev = 0;
     if (current_device(&dev) != TL_OK) return TL_EHIP;
-    std::lock_guard<std::mutex> lock(g_mu);
-    std::shared_ptr<StreamState>& sp = g_state[{dev, (void*)stream}];
-    if (!sp) {
-        sp = std::make_shared<StreamState>();
-        sp->dev = dev;
+    std::shared_ptr<StreamState> sp;
+    {
+        std::lock_guard<std::mutex> lock(g_mu);
+        std::shared_ptr<StreamState>& at = g_state[{dev, (void*)stream}];
+        if (!at) {
+            at = std::make_shared<StreamState>();
+            at->dev = dev;
+        }
+        sp = at;
     }
+    std::unique_lock<std::mutex> enqueue(sp->enqueue);
     StreamState& st = *sp;
     if (!st.fetch) {
         if (hipMalloc(&st.fetch, kStateWords * sizeof(unsigned long long)) != hipSuccess) { st.fetch = nullptr; return TL_ENOMEM; }
@@ -126,7 +138,8 @@ int get_state(hipStream_t stream, size_t ws_bytes, StateRef* out) {
         st.ws = p;
         st.ws_bytes = bytes;
     }
-    out->keep = sp;
+    out->keep = std::move(sp);
+    out->enqueue = std::move(enqueue);
     out->ws = st.ws;
     out->fetch = st.fetch;
     return TL_OK;
@@ -876,11 +889,12 @@ bool medium_grouped(const Plan& p, const tl_layout_desc* d, int64_t num_groups, 
 
 }  // namespace
 
-int stream_workspace(hipStream_t stream, size_t bytes, std::shared_ptr<void>* keep, void** ws) {
+int stream_workspace(hipStream_t stream, size_t bytes, StreamHold* hold, void** ws) {
     StateRef st;
     const int rc = get_state(stream, bytes, &st);
     if (rc != TL_OK) return rc;
-    *keep = st.keep;
+    hold->keep = std::move(st.keep);
+    hold->enqueue = std::move(st.enqueue);
     *ws = st.ws;
     return TL_OK;
 }
@@ -1273,6 +1287,7 @@ int tl_fetch_counter_read(void* stream, int64_t* bytes) {
     StateRef st;   // holds the tally's buffer for the rest of this call
     int rc = get_state(s, 0, &st);
     if (rc != TL_OK) return rc;
+    st.enqueue.unlock();    // what follows waits for the GPU
     unsigned long long v = 0;
     if (hipStreamSynchronize(s) != hipSuccess) return TL_EHIP;
     if (hipMemcpy(&v, st.fetch, sizeof v, hipMemcpyDeviceToHost) != hipSuccess) return TL_EHIP;

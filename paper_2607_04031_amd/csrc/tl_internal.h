@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <cstdint>
 #include <memory>
+#include <mutex>
 
 #include <hip/hip_runtime.h>
 
@@ -210,10 +211,14 @@ __host__ __device__ inline int64_t view_offset(const ViewProgram& P, int64_t e) 
     return off;
 }
 
-// At least 'bytes' of the stream's library workspace (grown by replacement),
-// alive as long as *keep; what it holds is the call's until the next call on
-// the stream.
-int stream_workspace(hipStream_t stream, size_t bytes, std::shared_ptr<void>* keep, void** ws);
+// At least 'bytes' of the stream's library workspace (grown by replacement):
+// it stays, and no other host thread's call enqueues work on it, as long as
+// *hold does, which a call keeps until its last launch is enqueued.
+struct StreamHold {
+    std::shared_ptr<void> keep;
+    std::unique_lock<std::mutex> enqueue;
+};
+int stream_workspace(hipStream_t stream, size_t bytes, StreamHold* hold, void** ws);
 
 // reads bytes (a multiple of 16) of src once and XORs its 32-bit words
 // into *checksum (one kernel; nothing for bytes = 0)

@@ -2,7 +2,6 @@
 // plan, dispatch.  Nothing is enqueued unless every check passes.
 #include <algorithm>
 #include <cmath>
-#include <memory>
 
 #include "tl_internal.h"
 #include "tl_serve.h"
@@ -240,10 +239,10 @@ int tl_attn(const void* Q, int64_t ldq, const tl_kv_cache* cache, const int32_t*
     a.out = static_cast<uint16_t*>(O);
     const int64_t floats = plan_attn(&a, D, cache->elem_bytes);
     if (a.max_tiles > kMaxGrid) return TL_EUNSUPPORTED;
-    std::shared_ptr<void> keep;
+    StreamHold hold;
     if (floats > 0) {
         void* ws = nullptr;
-        const int st = stream_workspace((hipStream_t)stream, size_t(floats) * 4, &keep, &ws);
+        const int st = stream_workspace((hipStream_t)stream, size_t(floats) * 4, &hold, &ws);
         if (st != TL_OK) return st;
         a.ws = static_cast<float*>(ws);
     }
@@ -280,8 +279,8 @@ int tl_verify(const void* logits, int32_t logits_dtype, int64_t vocab, const int
     a.path = path;
     a.counts = counts;
     a.next = next;
-    std::shared_ptr<void> keep;
-    const int st = stream_workspace((hipStream_t)stream, size_t(verify_workspace_bytes(vocab, total_nodes, num_seqs, max_nodes)), &keep, &a.ws);
+    StreamHold hold;
+    const int st = stream_workspace((hipStream_t)stream, size_t(verify_workspace_bytes(vocab, total_nodes, num_seqs, max_nodes)), &hold, &a.ws);
     if (st != TL_OK) return st;
     return done(launch_verify(a, (hipStream_t)stream));
 }
