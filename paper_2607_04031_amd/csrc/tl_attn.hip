@@ -266,7 +266,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
             for (int db = 0; db < D / 16; ++db)
                 *reinterpret_cast<f32x4v*>(o_s + ((wave * NT + nt) * 16 + col) * kPad + db * 16 + 4 * g) = o[nt][db];
         __syncthreads();
-        if (odd_any) {
+        const bool odd_here = odd_any;      // of all waves; read before a faster one may set it for its next piece
+        if (odd_here) {
             for (int c = piece.chunk0 + key_wave; c < chunk_end; c += kKeyWaves) {
                 const int64_t at = pages.block(c, pages.page(c, chunk_end));
                 if (c * kKeys + kKeys <= all || at < 0) continue;
@@ -291,11 +292,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 #pragma unroll
                 for (int j = 0; j < 8; ++j) x[j] += from[j] * f;
             }
-            if (odd_any) attn_add_odd(odd_s[row * (D / 8) + d / 8], x);
+            if (odd_here) attn_add_odd(odd_s[row * (D / 8) + d / 8], x);
             attn_put<D>(a, piece, row, d, x, top, sum);
         }
         __syncthreads();
-        if (odd_any) {          // uniform
+        if (odd_here) {         // uniform
             for (int i = threadIdx.x; i < kRows * (D / 8); i += kThreads) odd_s[i] = 0;
             __syncthreads();
             if (threadIdx.x == 0) odd_any = 0;
