@@ -65,8 +65,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
         // keys below 'all' are seen by every row of the wave, keys from 'end' on by none
         const int start = s.len - s.n, first_row = tile * kRows + row0;
         const int all = uniform(max(0, min(s.len, a.mask ? start : start + attn_token(a, first_row) + 1)));
-        const int end = uniform(max(0, min(s.len, a.mask ? s.len : start + min(s.n - 1, attn_token(a, first_row + 16 * NT - 1)) + 1)));
-        const int chunk_end = attn_token(a, first_row) >= s.n ? 0 : min(piece.chunk1, (end + kKeys - 1) / kKeys);
+        const int end = uniform(max(0, min(s.len, a.mask ? s.len : start + min(s.rows - 1, attn_token(a, first_row + 16 * NT - 1)) + 1)));
+        const int chunk_end = attn_token(a, first_row) >= s.rows ? 0 : min(piece.chunk1, (end + kKeys - 1) / kKeys);
 
         // this lane's rows: queries as the second operand of K Q^T, in the order of the keys' chunks
         u32x4 q[kQueriesInLds ? 1 : NT][kQueriesInLds ? 1 : kSteps];
@@ -76,7 +76,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
         for (int nt = 0; nt < NT; ++nt) {
             const int row = first_row + nt * 16 + col;
             own[nt] = attn_token(a, row);
-            const bool valid = own[nt] < s.n;
+            const bool valid = own[nt] < s.rows;
             const uint16_t* qp = a.q + int64_t(s.first + (valid ? own[nt] : 0)) * a.ldq + int64_t(head * a.group + (valid ? row - own[nt] * a.group : 0)) * D;
             if (!valid) own[nt] = -1;
 #pragma unroll
@@ -342,11 +342,11 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnLaunch a) {
     const int rows = 1 << a.log2_rows, floats = attn_partial_floats<D>(rows);
     const int c = threadIdx.x % kCols * 8, j = threadIdx.x / kCols % ROWS, part = threadIdx.x / (kCols * ROWS);
     const int row = blockIdx.y * ROWS + j, all_row = t.tile * rows + row, own = attn_token(a, all_row);
-    if (t.last < 0 || attn_token(a, t.tile * rows + int(blockIdx.y) * ROWS) >= t.n) return;
+    if (t.last < 0 || attn_token(a, t.tile * rows + int(blockIdx.y) * ROWS) >= t.rows) return;
     float top = -INFINITY, sum = 0.f, o[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i] = 0.f;
-    if (own < t.n) {
+    if (own < t.rows) {
 #pragma unroll 4
         for (int w = begin + part; w <= t.last; w += kParts) {
             const float* p = a.ws + (w == begin ? t.slot : 2 * int64_t(w)) * floats;
@@ -378,7 +378,7 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnLaunch a) {
             for (int i = 0; i < 8; ++i) o[i] = o[i] * f + o_s[x][j][c + i] * h;
         }
     }
-    if (own >= t.n) return;
+    if (own >= t.rows) return;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     u32x4 w;
 #pragma unroll

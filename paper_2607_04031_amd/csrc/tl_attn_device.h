@@ -28,6 +28,7 @@ __device__ inline void wait_for_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); } 
 constexpr int kTileCost = 96;
 struct Seq {
     int seq, first, n, len;     // first: row of the first new token; n: new tokens; len: keys
+    int rows;                   // new tokens that are computed: those within the caller's bound
     int tiles;                  // of rows
     int cost, rise;             // places of tile t: cost + (t + 1) rise
     int64_t before;             // places before the sequence
@@ -63,7 +64,8 @@ struct AttnLine {
 };
 
 __device__ inline void attn_sizes(const AttnLaunch& a, Seq* s) {
-    s->tiles = int((int64_t(s->n) * a.group + (1 << a.log2_rows) - 1) >> a.log2_rows);
+    s->rows = int(min(int64_t(s->n), a.max_q));      // the launch has workgroups for no more
+    s->tiles = int((int64_t(s->rows) * a.group + (1 << a.log2_rows) - 1) >> a.log2_rows);
     const bool rises = !a.mask && s->tiles > 1;
     s->rise = rises ? attn_token(a, 16 << a.log2_rows) >> a.log2_keys : 0;
     s->cost = (((rises ? max(0, s->len - s->n) : s->len) + (1 << a.log2_keys) - 1) >> a.log2_keys) * 16 + kTileCost;
@@ -177,7 +179,7 @@ __device__ inline int attn_by_xcd(int block, int groups) {
 template <int D>
 __host__ __device__ constexpr int attn_partial_floats(int rows) { return rows * (D + 2); }
 struct AttnShared {
-    int first, n, head, tile, last, slot;   // last < 0: none
+    int first, rows, head, tile, last, slot;    // last < 0: none
 };
 template <int D>
 __host__ __device__ constexpr int64_t attn_shared_at(int groups, int rows) { return 2 * int64_t(groups) * attn_partial_floats<D>(rows); }
@@ -234,7 +236,7 @@ __device__ inline AttnPiece attn_piece(const AttnLaunch& a, const AttnLine* line
         p.tile = p.s.tiles - 1 - uniform(int(in_seq - int64_t(p.head) * p.s.tiles));    // the longest first
     }
     // chunks that some row of the tile sees
-    const int last = min(p.s.n - 1, attn_token(a, ((p.tile + 1) << a.log2_rows) - 1));
+    const int last = min(p.s.rows - 1, attn_token(a, ((p.tile + 1) << a.log2_rows) - 1));
     const int end = a.mask ? p.s.len : max(0, min(p.s.len, p.s.len - p.s.n + last + 1));
     const int chunks = (end + (1 << a.log2_keys) - 1) >> a.log2_keys;
     p.chunk0 = 0;
@@ -253,7 +255,7 @@ __device__ inline AttnPiece attn_piece(const AttnLaunch& a, const AttnLine* line
     p.slot = 2 * int64_t(r->me) + (start > r->place0 ? 1 : 0);
     r->place = start + to;
     if (start >= r->place0 && to < places && threadIdx.x == 0)      // others go on with it
-        attn_shared<D>(a)[r->me] = AttnShared{p.s.first, p.s.n, p.head, p.tile, attn_group_of(start + places - 1, r->total, r->groups), int(p.slot)};
+        attn_shared<D>(a)[r->me] = AttnShared{p.s.first, p.s.rows, p.head, p.tile, attn_group_of(start + places - 1, r->total, r->groups), int(p.slot)};
     return p;
 }
 
@@ -274,7 +276,7 @@ struct AttnPages {
 template <int D>
 __device__ inline void attn_put(const AttnLaunch& a, const AttnPiece& p, int row, int d, const float (&o)[8], float m, float l) {
     const int rows = 1 << a.log2_rows, at = (p.tile << a.log2_rows) + row, i = attn_token(a, at);
-    if (i >= p.s.n) return;
+    if (i >= p.s.rows) return;
     if (p.whole) {
         const float inv = l == 0.f ? 0.f : 1.f / l;    // a row that sees no key: zeros
         u32x4 w;
@@ -337,7 +339,7 @@ template <int D, int ELEM, int MB>
 __device__ inline void attn_odd_chunk(const AttnLaunch& a, const AttnPiece& p, int c, int64_t block, int row, uint32_t* odd) {
     const int lane = threadIdx.x & 63, g = lane >> 4, i = attn_token(a, (p.tile << a.log2_rows) + row);
     const int key0 = c * (16 * MB) + 4 * g, left = p.s.len - key0;
-    const uint32_t seen = i < p.s.n ? attn_seen<MB>(a, p.s, i, key0 - (p.s.len - p.s.n), left) : 0u;
+    const uint32_t seen = i < p.s.rows ? attn_seen<MB>(a, p.s, i, key0 - (p.s.len - p.s.n), left) : 0u;
 #pragma unroll 1
     for (int step = 0; step < 3 * (D / 16) * (MB / 2); ++step) {
         const int kind = step % 3, db = step / 3 % (D / 16), h = step / 3 / (D / 16);

@@ -71,7 +71,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
         const int start = s.len - s.n;
         auto all_of = [&](int first) { return max(0, min(s.len, a.mask ? start : start + attn_token(a, first) + 1)); };
         auto end_of = [&](int first, int count) {
-            return attn_token(a, first) >= s.n ? 0 : max(0, min(s.len, a.mask ? s.len : start + min(s.n - 1, attn_token(a, first + count - 1)) + 1));
+            return attn_token(a, first) >= s.rows ? 0 : max(0, min(s.len, a.mask ? s.len : start + min(s.rows - 1, attn_token(a, first + count - 1)) + 1));
         };
         const int first_row = piece.tile * kRows + row0;
         const int all_here = uniform(all_of(piece.tile * kRows)), all = uniform(all_of(first_row));
@@ -85,7 +85,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
         for (int nt = 0; nt < kRowTiles; ++nt) {
             const int row = first_row + nt * 16 + col;
             own[nt] = attn_token(a, row);
-            const bool valid = own[nt] < s.n;
+            const bool valid = own[nt] < s.rows;
             const uint16_t* qp = a.q + int64_t(s.first + (valid ? own[nt] : 0)) * a.ldq + int64_t(piece.head * a.group + (valid ? row - own[nt] * a.group : 0)) * D;
             if (!valid) own[nt] = -1;
 #pragma unroll
