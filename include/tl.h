@@ -595,7 +595,9 @@ enum { TL_IN_F32 = 0, TL_IN_BF16 = 1 };
  * q_heads, a row stride below a row's length or not a multiple of 16 bytes, a
  * bad in_dtype or rope, outputs that overlap inputs or each other;
  * TL_EUNSUPPORTED for q_heads above 4096, row strides above 2^30, or n rows
- * whose heads need more than 2^31 - 1 workgroups.  n == 0 enqueues nothing.
+ * that need 2^24 workgroups or more (a launch's limit of 2^32 work-items; one
+ * row's queries, 16 rows' keys and 64 rows' values of a head are one each at
+ * most).  n == 0 enqueues nothing.
  */
 int tl_kv_append(const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv,
                  int32_t in_dtype, int64_t n, int32_t q_heads, const int32_t* slots,
@@ -608,8 +610,8 @@ int tl_kv_append(const void* Q, int64_t ldq, const void* K, int64_t ldk, const v
  * subnormal bf16).  A slot outside the cache reads zeros.  Either output may
  * be NULL.  Errors: TL_EINVAL for a bad cache, NULL or misaligned pointers,
  * n < 0, both outputs NULL, or outputs that overlap the cache, slots or each
- * other; TL_EUNSUPPORTED for more than 2^31 - 1 workgroups.  n == 0 enqueues
- * nothing.
+ * other; TL_EUNSUPPORTED for 2^24 workgroups or more (64 rows of a head are
+ * one).  n == 0 enqueues nothing.
  */
 int tl_kv_read(const tl_kv_cache* cache, const int32_t* slots, int64_t n, void* K_out, void* V_out, void* stream);
 
@@ -630,7 +632,7 @@ int tl_kv_read(const tl_kv_cache* cache, const int32_t* slots, int64_t n, void* 
  * Sequences must not share the pages that hold their new tokens.
  * Errors: TL_EINVAL for a bad cache, NULL or misaligned pointers (4 bytes),
  * num_seqs < 0, max_pages < 1, max_path < 1; TL_EUNSUPPORTED for max_path
- * above 4096 or num_seqs * kv_heads above 2^31 - 1.  num_seqs == 0 enqueues
+ * above 4096 or num_seqs * kv_heads of 2^24 or more.  num_seqs == 0 enqueues
  * nothing.
  */
 int tl_kv_keep(const tl_kv_cache* cache, const int32_t* page_table, int64_t max_pages, const int32_t* starts,
@@ -674,9 +676,9 @@ int tl_kv_keep(const tl_kv_cache* cache, const int32_t* page_table, int64_t max_
  * bytes, the rest 4), negative counts, max_pages < 1, q_heads not a positive
  * multiple of kv_heads, a bad ldq (see tl_kv_append) or scale, mask_words < 1
  * with a mask, or O overlapping an input; TL_EUNSUPPORTED for max_len or
- * total_q * q_heads above 2^30, mask_words above 2^16, ldq above 2^30 or a
- * grid above 2^31 - 1 workgroups; TL_ENOMEM if the workspace cannot be
- * allocated.  total_q == 0 or num_seqs == 0 enqueues nothing.
+ * total_q * q_heads above 2^30, mask_words above 2^16, ldq above 2^30 or
+ * 2^24 workgroups or more (a tile of 16 to 128 rows each); TL_ENOMEM if the
+ * workspace cannot be allocated.  total_q == 0 or num_seqs == 0 enqueues nothing.
  */
 int tl_attn(const void* Q, int64_t ldq, const tl_kv_cache* cache, const int32_t* page_table, int64_t max_pages,
             const int32_t* lens, const int32_t* q_offsets, const uint32_t* mask, int32_t mask_words,
@@ -722,8 +724,9 @@ int tl_attn(const void* Q, int64_t ldq, const tl_kv_cache* cache, const int32_t*
  * workspace of the stream (see "HIP graphs" above).
  * Errors: TL_EINVAL for NULL or misaligned pointers (logits, draft, noise 16
  * bytes, the rest 4), vocab < 1, negative counts, max_nodes < 1 or a bad
- * dtype; TL_EUNSUPPORTED for vocab or total_nodes above 2^26 or max_nodes
- * above 4096; TL_ENOMEM as above.  num_seqs == 0 enqueues nothing.
+ * dtype; TL_EUNSUPPORTED for vocab above 2^26, total_nodes of 2^24 or more,
+ * num_seqs of 2^22 or more or max_nodes above 4096; TL_ENOMEM as above.
+ * num_seqs == 0 enqueues nothing.
  */
 int tl_verify(const void* logits, int32_t logits_dtype, int64_t vocab, const int32_t* node_offsets,
               const int32_t* parents, const int32_t* tokens, int32_t num_seqs, int64_t total_nodes,

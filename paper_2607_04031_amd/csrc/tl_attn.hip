@@ -30,6 +30,7 @@ namespace {
 
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
+static_assert(kThreads == kAttnThreads, "the limit of a launch's workgroups");
 constexpr float kSlack = 8.f;
 
 template <int D, int ELEM, int NT, int RG>

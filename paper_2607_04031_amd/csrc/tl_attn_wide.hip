@@ -22,6 +22,7 @@ namespace {
 
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
+static_assert(kThreads == kAttnThreads, "the limit of a launch's workgroups");
 constexpr int kRowTiles = 2;            // of 16 rows, a wave's
 constexpr int kRows = 16 * kRowTiles * kWaves;
 constexpr int kKeys = 64;

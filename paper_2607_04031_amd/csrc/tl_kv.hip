@@ -11,7 +11,7 @@
 namespace tl {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = kKvThreads;
 
 // Where a token's entries lie: its page (valid, or negative) and place in it.
 __device__ inline int64_t page_of(const KvView& c, int slot, int* t) {
@@ -551,26 +551,28 @@ __global__ __launch_bounds__(kThreads) void kv_keep_kernel(KvKeepLaunch a) {
 // 512 10.4 and 8.5, 8192 119 and 72; read, 512 3.4 and 4.0, 1024 4.5 and 4.2, 8192 22.8 and 10.7.
 constexpr int64_t kAppendWindowRows = 512, kReadWindowRows = 1024;
 
+// All workgroups; *b: in windows.
+int64_t append_blocks(const KvAppendLaunch& a, int D, AppendBlocks* b) {
+    const int per = kThreads / (D / 8);
+    if (a.n < kAppendWindowRows) return a.n * ((a.heads[0] + a.heads[1] + a.heads[2] + per - 1) / per);
+    // one window more than the rows need: the first one may begin inside.  A workgroup takes all heads (their angles
+    // once) where the rows alone are enough for the CUs, otherwise as few as it can
+    const bool many = a.n >= 2048;
+    b->key_heads = many ? std::max(1, a.heads[1]) : std::max(1, per / kKeyWindow);
+    b->query_heads = many ? std::max(1, a.heads[0]) : per;
+    const int64_t keys = ((a.n + kKeyWindow - 1) / kKeyWindow + 1) * ((a.heads[1] + b->key_heads - 1) / b->key_heads);
+    const int64_t values = a.heads[2] * ((a.n + kValueWindow - 1) / kValueWindow + 1);
+    b->keys = int(keys);
+    b->values = int(values);
+    return keys + values + a.n * ((a.heads[0] + b->query_heads - 1) / b->query_heads);
+}
+
 template <int D, int ELEM, bool F32>
 hipError_t append_from(const KvAppendLaunch& a, hipStream_t stream) {
-    if (a.n >= kAppendWindowRows) {
-        // one window more than the rows need: the first one may begin inside.  A workgroup takes all heads (their angles
-        // once) where the rows alone are enough for the CUs, otherwise as few as it can
-        const int per = kThreads / (D / 8), key_per = std::max(1, per / kKeyWindow);
-        const bool many = a.n >= 2048;
-        AppendBlocks b{};
-        b.key_heads = many ? std::max(1, a.heads[1]) : key_per;
-        b.query_heads = many ? std::max(1, a.heads[0]) : per;
-        const int64_t keys = ((a.n + kKeyWindow - 1) / kKeyWindow + 1) * ((a.heads[1] + b.key_heads - 1) / b.key_heads);
-        const int64_t values = a.heads[2] * ((a.n + kValueWindow - 1) / kValueWindow + 1);
-        const int64_t queries = a.n * ((a.heads[0] + b.query_heads - 1) / b.query_heads);
-        b.keys = int(keys);
-        b.values = int(values);
-        hipLaunchKernelGGL((kv_append_window_kernel<D, ELEM, F32>), dim3(uint32_t(keys + values + queries)), dim3(kThreads), 0, stream, a, b);
-    } else {
-        const int per = kThreads / (D / 8), blocks = (a.heads[0] + a.heads[1] + a.heads[2] + per - 1) / per;
-        hipLaunchKernelGGL((kv_append_kernel<D, ELEM, F32>), dim3(uint32_t(a.n * blocks)), dim3(kThreads), 0, stream, a, blocks);
-    }
+    AppendBlocks b{};
+    const uint32_t blocks = uint32_t(append_blocks(a, D, &b));
+    if (a.n >= kAppendWindowRows) hipLaunchKernelGGL((kv_append_window_kernel<D, ELEM, F32>), dim3(blocks), dim3(kThreads), 0, stream, a, b);
+    else hipLaunchKernelGGL((kv_append_kernel<D, ELEM, F32>), dim3(blocks), dim3(kThreads), 0, stream, a, int(blocks / a.n));
     return hipGetLastError();
 }
 
@@ -581,13 +583,9 @@ hipError_t append_as(const KvAppendLaunch& a, hipStream_t stream) {
 
 template <int D, int ELEM>
 hipError_t read_as(const KvView& c, const int32_t* slots, int64_t n, uint16_t* k_out, uint16_t* v_out, hipStream_t stream) {
-    if (n >= kReadWindowRows) {
-        const uint32_t blocks = uint32_t((n + kValueWindow - 1) / kValueWindow + 1) * c.heads;
-        hipLaunchKernelGGL((kv_read_window_kernel<D, ELEM>), dim3(blocks), dim3(kThreads), 0, stream, c, slots, n, k_out, v_out);
-    } else {
-        const int64_t lanes = n * c.heads * (D / 8);
-        hipLaunchKernelGGL((kv_read_kernel<D, ELEM>), dim3(uint32_t((lanes + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, c, slots, n, k_out, v_out);
-    }
+    const uint32_t blocks = uint32_t(kv_read_workgroups(c, D, n));
+    if (n >= kReadWindowRows) hipLaunchKernelGGL((kv_read_window_kernel<D, ELEM>), dim3(blocks), dim3(kThreads), 0, stream, c, slots, n, k_out, v_out);
+    else hipLaunchKernelGGL((kv_read_kernel<D, ELEM>), dim3(blocks), dim3(kThreads), 0, stream, c, slots, n, k_out, v_out);
     return hipGetLastError();
 }
 
@@ -598,6 +596,15 @@ hipError_t keep_as(const KvKeepLaunch& a, hipStream_t stream) {
 }
 
 }  // namespace
+
+int64_t kv_append_workgroups(const KvAppendLaunch& a, int head_dim) {
+    AppendBlocks b{};
+    return append_blocks(a, head_dim, &b);
+}
+
+int64_t kv_read_workgroups(const KvView& c, int head_dim, int64_t n) {
+    return n >= kReadWindowRows ? ((n + kValueWindow - 1) / kValueWindow + 1) * c.heads : (n * c.heads * (head_dim / 8) + kThreads - 1) / kThreads;
+}
 
 hipError_t launch_kv_append(const KvAppendLaunch& a, int head_dim, int elem_bytes, hipStream_t stream) {
     if (head_dim == 64) return elem_bytes == 1 ? append_as<64, 1>(a, stream) : append_as<64, 2>(a, stream);

@@ -9,7 +9,7 @@
 namespace tl {
 namespace {
 
-constexpr int64_t kMaxGrid = 0x7fffffff;
+constexpr int64_t kMaxInt = 0x7fffffff;
 constexpr int64_t kMaxStride = int64_t(1) << 30;
 constexpr int kMaxNodes = 4096;
 
@@ -30,7 +30,7 @@ bool overlap(const Range& a, const Range& b) {
 int check_sizes(const tl_kv_cache* c, int64_t* data, int64_t* exps) {
     if (!c || c->num_pages < 1 || !is_pow2(c->page_tokens) || c->page_tokens < 64 || c->page_tokens > 4096) return TL_EINVAL;
     if (c->kv_heads < 1 || c->kv_heads > 1024 || (c->elem_bytes != 1 && c->elem_bytes != 2)) return TL_EINVAL;
-    if (c->num_pages > kMaxGrid / c->page_tokens) return TL_EINVAL;
+    if (c->num_pages > kMaxInt / c->page_tokens) return TL_EINVAL;
     if (c->head_dim != 64 && c->head_dim != 128) return TL_EUNSUPPORTED;
     const int64_t tokens = c->num_pages * c->page_tokens * c->kv_heads;
     *data = tokens * c->head_dim * c->elem_bytes;
@@ -86,7 +86,7 @@ int64_t plan_attn(AttnLaunch* a, int head_dim, int elem_bytes) {
     const int64_t whole = rows > 16 ? 1024 : elem_bytes == 1 ? 2048 : 1536;
     const bool enough = wide ? a->mask && a->max_tiles >= 2 * kSlots && a->max_len <= 2048 : a->max_tiles >= kSlots && a->max_len <= 4096;
     a->split = a->max_len > whole && !enough && a->max_tiles < 4 * kSlots;
-    a->groups = int(a->split ? kSlots : std::min<int64_t>(a->max_tiles, kMaxGrid));
+    a->groups = int(a->split ? kSlots : a->max_tiles);
     return a->split ? 2 * a->groups * rows * (head_dim + 2) + a->groups * 8 : 0;
 }
 
@@ -115,6 +115,7 @@ int tl_kv_append(const void* Q, int64_t ldq, const void* K, int64_t ldk, const v
     if (rc != TL_OK) return rc;
     if (n < 0 || q_heads < 0 || (in_dtype != TL_IN_F32 && in_dtype != TL_IN_BF16)) return TL_EINVAL;
     if (n == 0) return TL_OK;
+    a.n = n;
     if ((K == nullptr) != (V == nullptr) || (Q == nullptr) != (q_heads == 0) || (Q == nullptr) != (Q_out == nullptr)) return TL_EINVAL;
     if (!Q && !K) return TL_EINVAL;
     if (q_heads > 4096) return TL_EUNSUPPORTED;
@@ -148,8 +149,7 @@ int tl_kv_append(const void* Q, int64_t ldq, const void* K, int64_t ldk, const v
         a.rot_dim = rope->rot_dim;
         a.interleaved = rope->interleaved != 0;
     }
-    const int64_t all = int64_t(heads[0]) + heads[1] + heads[2];
-    if (n > kMaxGrid / all) return TL_EUNSUPPORTED;
+    if (n > kMaxInt || kv_append_workgroups(a, D) > most_workgroups(kKvThreads)) return TL_EUNSUPPORTED;
     const Range out = {Q_out, n * q_heads * D * 2};
     for (int i = 0; i < 3; ++i) {
         const Range r = {src[i], span(n, ld[i], int64_t(heads[i]) * D, in)};
@@ -157,7 +157,6 @@ int tl_kv_append(const void* Q, int64_t ldq, const void* K, int64_t ldk, const v
     }
     if (K && hits_cache(cache, data, exps, out)) return TL_EINVAL;
     a.src_f32 = in_dtype == TL_IN_F32;
-    a.n = n;
     a.q_out = static_cast<uint16_t*>(Q_out);
     return done(launch_kv_append(a, D, cache->elem_bytes, (hipStream_t)stream));
 }
@@ -171,7 +170,7 @@ int tl_kv_read(const tl_kv_cache* cache, const int32_t* slots, int64_t n, void* 
     if (n == 0) return TL_OK;
     if (bad_pointer(slots, 4) || (!K_out && !V_out) || !aligned(K_out, 16) || !aligned(V_out, 16)) return TL_EINVAL;
     const int64_t row = int64_t(cache->kv_heads) * cache->head_dim;
-    if (n > kMaxGrid / (row / 8) * 256) return TL_EUNSUPPORTED;
+    if (n > kMaxInt || kv_read_workgroups(view, cache->head_dim, n) > most_workgroups(kKvThreads)) return TL_EUNSUPPORTED;
     const Range k = {K_out, n * row * 2}, v = {V_out, n * row * 2}, s = {slots, n * 4};
     if (overlap(k, v) || overlap(k, s) || overlap(v, s)) return TL_EINVAL;
     if (hits_cache(cache, data, exps, k) || hits_cache(cache, data, exps, v)) return TL_EINVAL;
@@ -188,7 +187,7 @@ int tl_kv_keep(const tl_kv_cache* cache, const int32_t* page_table, int64_t max_
     if (num_seqs < 0 || max_pages < 1 || max_path < 1) return TL_EINVAL;
     if (num_seqs == 0) return TL_OK;
     if (bad_pointer(page_table, 4) || bad_pointer(starts, 4) || bad_pointer(path, 4) || bad_pointer(counts, 4)) return TL_EINVAL;
-    if (max_path > kMaxNodes || num_seqs > kMaxGrid / cache->kv_heads) return TL_EUNSUPPORTED;
+    if (max_path > kMaxNodes || num_seqs > most_workgroups(kKvThreads) / cache->kv_heads) return TL_EUNSUPPORTED;
     a.page_table = page_table;
     a.max_pages = max_pages;
     a.starts = starts;
@@ -217,7 +216,7 @@ int tl_attn(const void* Q, int64_t ldq, const tl_kv_cache* cache, const int32_t*
     }
     if (ldq > kMaxStride || max_len > kMaxStride || q_heads > kMaxStride / std::max<int64_t>(total_q, 1) || (mask && mask_words > 65536)) return TL_EUNSUPPORTED;
     if (total_q == 0 || num_seqs == 0 || max_q == 0) return TL_OK;
-    if (max_pages > kMaxGrid) return TL_EUNSUPPORTED;
+    if (max_pages > kMaxInt) return TL_EUNSUPPORTED;
     const Range out = {O, total_q * width * 2};
     if (overlap(out, {Q, span(total_q, ldq, width, 2)}) || hits_cache(cache, data, exps, out) ||
         overlap(out, {mask, total_q * mask_words * 4}) || overlap(out, {page_table, num_seqs * max_pages * 4}) ||
@@ -238,7 +237,7 @@ int tl_attn(const void* Q, int64_t ldq, const tl_kv_cache* cache, const int32_t*
     a.scale_log2 = scale * 1.44269504088896340736f;
     a.out = static_cast<uint16_t*>(O);
     const int64_t floats = plan_attn(&a, D, cache->elem_bytes);
-    if (a.max_tiles > kMaxGrid) return TL_EUNSUPPORTED;
+    if (a.max_tiles > most_workgroups(kAttnThreads)) return TL_EUNSUPPORTED;
     StreamHold hold;
     if (floats > 0) {
         void* ws = nullptr;
@@ -260,7 +259,7 @@ int tl_verify(const void* logits, int32_t logits_dtype, int64_t vocab, const int
     if (bad_pointer(node_offsets, 4) || bad_pointer(temperature, 4) || bad_pointer(path, 4) || bad_pointer(counts, 4) || bad_pointer(next, 4)) return TL_EINVAL;
     if (bad_pointer(noise, 16) || !aligned(draft, 16)) return TL_EINVAL;
     if (total_nodes > 0 && (bad_pointer(logits, 16) || bad_pointer(parents, 4) || bad_pointer(tokens, 4) || bad_pointer(uniform, 4))) return TL_EINVAL;
-    if (vocab > (1 << 26) || total_nodes > (1 << 26) || max_nodes > kMaxNodes || num_seqs > (1 << 24)) return TL_EUNSUPPORTED;
+    if (vocab > (1 << 26) || total_nodes > kMostVerifyNodes || num_seqs > kMostVerifySeqs || max_nodes > kMaxNodes) return TL_EUNSUPPORTED;
     VerifyLaunch a{};
     a.logits = logits;
     a.logits_bf16 = logits_dtype == TL_OUT_BF16;

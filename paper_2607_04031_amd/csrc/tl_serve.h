@@ -46,6 +46,10 @@ __host__ __device__ inline int kv_value_at(int t, int d) {
 __host__ __device__ inline int kv_key_exp_at(int t) { return (t & ~63) + (t & 15) * 4 + ((t & 63) >> 4); }
 __host__ __device__ inline int kv_value_exp_at(int t) { return (t & ~63) + ((t & 15) >> 2) * 16 + ((t & 63) >> 4) * 4 + (t & 3); }
 
+// Workgroups of a launch, at most: HIP takes fewer than 2^32 work-items in a
+// dimension.  The entry points refuse a call with more in any of its launches.
+constexpr int64_t most_workgroups(int threads) { return ((int64_t(1) << 32) - 1) / threads; }
+
 struct KvAppendLaunch {
     KvView c;
     const void* src[3];       // queries, keys, values: rows of heads * D elements
@@ -61,8 +65,11 @@ struct KvAppendLaunch {
     bool interleaved;
     uint16_t* q_out;          // bf16 [n][heads[0]][D]
 };
+constexpr int kKvThreads = 256;
+int64_t kv_append_workgroups(const KvAppendLaunch& a, int head_dim);
 hipError_t launch_kv_append(const KvAppendLaunch& a, int head_dim, int elem_bytes, hipStream_t stream);
 
+int64_t kv_read_workgroups(const KvView& c, int head_dim, int64_t n);
 hipError_t launch_kv_read(const KvView& c, int head_dim, int elem_bytes, const int32_t* slots, int64_t n, uint16_t* k_out,
                           uint16_t* v_out, hipStream_t stream);
 
@@ -107,6 +114,7 @@ struct AttnLaunch {
     int groups;
     float* ws;                // partial results: two per workgroup (split)
 };
+constexpr int kAttnThreads = 256;
 // Fills the plan; returns the workspace it needs, in floats.
 int64_t plan_attn(AttnLaunch* a, int head_dim, int elem_bytes);
 hipError_t launch_attn(const AttnLaunch& a, int head_dim, int elem_bytes, hipStream_t stream);
@@ -133,6 +141,8 @@ struct VerifyLaunch {
     int32_t* next;
     void* ws;
 };
+// rows with a workgroup of 256 threads or more each, sequences with one of 1024
+constexpr int64_t kMostVerifyNodes = most_workgroups(256), kMostVerifySeqs = most_workgroups(1024);
 int64_t verify_workspace_bytes(int64_t vocab, int64_t total, int num_seqs, int max_nodes);
 hipError_t launch_verify(const VerifyLaunch& a, hipStream_t stream);
 

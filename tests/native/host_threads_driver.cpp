@@ -71,6 +71,8 @@ hipError_t launch_view_load(const uint8_t*, int64_t, const ViewProgram&, uint8_t
 hipError_t launch_zero_u64(unsigned long long* p, hipStream_t) { std::memset(p, 0, kStateWords * sizeof *p); return hipSuccess; }
 hipError_t launch_stream_read(const uint8_t*, int64_t, unsigned*, hipStream_t) { std::abort(); }
 hipError_t scratch_address(float**) { std::abort(); }
+int64_t kv_append_workgroups(const KvAppendLaunch&, int) { std::abort(); }
+int64_t kv_read_workgroups(const KvView&, int, int64_t) { std::abort(); }
 hipError_t launch_kv_append(const KvAppendLaunch&, int, int, hipStream_t) { std::abort(); }
 hipError_t launch_kv_read(const KvView&, int, int, const int32_t*, int64_t, uint16_t*, uint16_t*, hipStream_t) { std::abort(); }
 hipError_t launch_kv_keep(const KvKeepLaunch&, int, int, hipStream_t) { std::abort(); }
