@@ -150,12 +150,17 @@ int tl_kv_append(const void* Q, int64_t ldq, const void* K, int64_t ldk, const v
         a.interleaved = rope->interleaved != 0;
     }
     if (n > kMaxInt || kv_append_workgroups(a, D) > most_workgroups(kKvThreads)) return TL_EUNSUPPORTED;
-    const Range out = {Q_out, n * q_heads * D * 2};
-    for (int i = 0; i < 3; ++i) {
-        const Range r = {src[i], span(n, ld[i], int64_t(heads[i]) * D, in)};
-        if (overlap(out, r) || (K && hits_cache(cache, data, exps, r))) return TL_EINVAL;
-    }
+    // outputs: the queries and the cache's arrays (no part of this call without keys)
+    const Range out = {Q_out, n * q_heads * D * 2}, arrays[4] = {{cache->k, data}, {cache->v, data}, {cache->k_exp, exps}, {cache->v_exp, exps}};
+    auto hit = [&](const Range& r) { return overlap(out, r) || (K && hits_cache(cache, data, exps, r)); };
+    for (int i = 0; i < 3; ++i)
+        if (hit({src[i], span(n, ld[i], int64_t(heads[i]) * D, in)})) return TL_EINVAL;
+    if (hit({a.slots, n * 4})) return TL_EINVAL;
+    if (rope && (hit({rope->positions, n * rope->axes * 4}) || hit({rope->inv_freq, rope->rot_dim / 2 * 4}))) return TL_EINVAL;
     if (K && hits_cache(cache, data, exps, out)) return TL_EINVAL;
+    for (int i = 0; K && i < 4; ++i)
+        for (int j = 0; j < i; ++j)
+            if (overlap(arrays[i], arrays[j])) return TL_EINVAL;
     a.src_f32 = in_dtype == TL_IN_F32;
     a.q_out = static_cast<uint16_t*>(Q_out);
     return done(launch_kv_append(a, D, cache->elem_bytes, (hipStream_t)stream));
