@@ -125,9 +125,13 @@ class RopeDesc(ctypes.Structure):
 
 class KVCache:
     """tl_kv_cache over tensors that it keeps alive: k and v [pages, kv_heads, page_tokens * head_dim] (uint8 holding
-    E4M3, or bfloat16), k_exp and v_exp uint8 [pages, kv_heads, page_tokens] (None for bfloat16)."""
+    E4M3, float8_e4m3fn or bfloat16), k_exp and v_exp uint8 [pages, kv_heads, page_tokens] (None for bfloat16)."""
 
     def __init__(self, k, v, k_exp, v_exp, page_tokens, kv_heads, head_dim):
+        import torch
+        if any(x.dtype not in (torch.uint8, torch.float8_e4m3fn, torch.bfloat16) for x in (k, v)) or \
+                any(x is not None and x.dtype != torch.uint8 for x in (k_exp, v_exp)):
+            raise ValueError("k and v are uint8 or float8_e4m3fn (E4M3), or bfloat16, exponents uint8")
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
         self.page_tokens, self.kv_heads, self.head_dim = page_tokens, kv_heads, head_dim
         self.elem_bytes = k.element_size()
@@ -138,7 +142,7 @@ class KVCache:
         if (k_exp is None) != (self.elem_bytes == 2) or (v_exp is None) != (self.elem_bytes == 2):
             raise ValueError("8-bit caches have exponents, and only they")
         for x in (k_exp, v_exp):
-            if x is not None and (x.element_size() != 1 or x.numel() != self.num_pages * page_tokens * kv_heads):
+            if x is not None and (x.numel() != self.num_pages * page_tokens * kv_heads):
                 raise ValueError("one exponent byte per token and head")
         self.desc = KVCacheDesc(_ptr(k), _ptr(v), _ptr(k_exp), _ptr(v_exp), self.num_pages, page_tokens, kv_heads,
                                 head_dim, self.elem_bytes)
