@@ -16,6 +16,14 @@ __device__ inline f32x4v mfma_16x16x32(u32x4 a, u32x4 b, f32x4v c) {
 // entry, the compiler has every pass through it wait for all loads instead.
 __device__ inline void wait_for_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }    // vmcnt 0
 
+// The same before reads of LDS that such loads write past the registers: the
+// statement says that memory is another one, so that no read moves before the
+// wait, whatever the builtin is taken to touch.
+__device__ inline void wait_for_lds_loads() {
+    wait_for_loads();
+    asm volatile("" ::: "memory");
+}
+
 // The work is a line: sequence after sequence, in it head after head, in it
 // tile after tile of rows.  Without a split a workgroup takes one tile of a
 // head.  With one, a tile takes as many places as it costs, in sixteenths of a

@@ -30,7 +30,8 @@ constexpr float kSlack = 8.f;
 
 // 16 bytes a lane from global memory (base + voff) to LDS, at the wave's base in the order of the lanes, past the
 // registers.  In assembly, since the compiler has every later read of LDS wait for such loads, also one of another buffer;
-// wait_for_loads() and a barrier stand before the reads that they are for.  Nothing else in the kernels uses M0.
+// wait_for_lds_loads(), and a barrier for other waves, stand before the reads that they are for.  Nothing else in the
+// kernels uses M0.
 __device__ inline void load_to_lds(const uint8_t* base, uint32_t voff, u32x4* lds) {
     const uint32_t la = uint32_t(uintptr_t((__attribute__((address_space(3))) void*)lds));
 #pragma clang diagnostic push
@@ -287,11 +288,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
         int next_page = pages.page(piece.chunk0 + 2, chunk_end);
         if (piece.chunk0 < chunk_end) {
             fetch(block, 0);
-            if (ELEM == 2) wait_for_loads();
+            if (ELEM == 2) wait_for_lds_loads();
             put(std::true_type(), 0, piece.chunk0);
             if (ELEM == 1) fetch(next, 0);
         }
-        wait_for_loads();
+        wait_for_lds_loads();
         __syncthreads();
         // chunks that all rows see whole, and the next one too; then the others
         int chunk = piece.chunk0;
@@ -306,7 +307,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
                 if (ELEM == 1 || more) fetch(kAhead == 2 ? after : next, buffer ^ 1);
                 if (block >= 0 && (!kMasked || chunk < wave_end)) compute(may_mask, buffer, chunk);
                 if (ELEM == 2) {
-                    wait_for_loads();
+                    wait_for_lds_loads();
                     if (kMasked && more) put(may_mask, buffer ^ 1, chunk + 1);
                 }
                 block = next;
