@@ -176,7 +176,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
                     // among the others for now: 0 * NaN would reach rows that do not see the key
                     if (part == 0) {
 #pragma unroll
-                        for (int mb = 0; mb < kBlocks; ++mb) v_exp[mb] &= attn_first_bytes(left - 16 * mb);
+                        for (int mb = 0; mb < kBlocks; ++mb) {
+                            v_exp[mb] &= attn_first_bytes(left - 16 * mb);
+                            v_exp[mb] -= attn_full_bytes(v_exp[mb]);
+                        }
 #pragma unroll
                         for (int i = 0; i < kLoads; ++i)
 #pragma unroll

@@ -327,6 +327,11 @@ __device__ inline uint32_t attn_seen(const AttnLaunch& a, const Seq& s, int own,
 __device__ inline uint32_t attn_first_bytes(int n) { return n <= 0 ? 0u : n >= 4 ? ~0u : (1u << (8 * n)) - 1; }
 __device__ inline uint32_t attn_first_halves(int n) { return n <= 0 ? 0u : n >= 2 ? ~0u : 0xffffu; }
 
+// 1 in those of a word's bytes that are 0xff: less that, they are scales of
+// 2^127 and not of infinity, of which 0 times is 0.  No entry that was written
+// has such a scale; one that was not may have any, and rows need not see it.
+__device__ inline uint32_t attn_full_bytes(uint32_t w) { return (((w & 0x7f7f7f7fu) + 0x01010101u) & w & 0x80808080u) >> 7; }
+
 // all ones in those of a word's four E4M3 or two bf16 values that are no finite numbers
 template <int ELEM>
 __device__ inline uint32_t attn_odd(uint32_t w) {

@@ -175,7 +175,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
                     vs[(2 * at + h) * 64] = u32x4{fp8_to_bf16<false>(v0, 1.f), fp8_to_bf16<true>(v0, 1.f), fp8_to_bf16<false>(v1, 1.f), fp8_to_bf16<true>(v1, 1.f)};
                 }
             }
-            if (thread < kKeys) scale_s[buffer][thread] = exp_scale(v_exp);
+            if (thread < kKeys) scale_s[buffer][thread] = exp_scale(min(v_exp, 0xfeu));    // as attn_full_bytes
         };
         // Operands are read from LDS four ahead of the products that take them: left to itself, the compiler reads one
         // and waits for it, twenty times a chunk.  A wave in its products goes before the other one of its SIMD (8 bits: 1 - 2 %
