@@ -4,6 +4,7 @@ _tl_torch.so (host code that takes torch tensors to it) with the C++ compiler.
     python -m paper_2607_04031_amd.build          # or build() from Python
 """
 import os
+import shutil
 import subprocess
 import sys
 import sysconfig
@@ -36,7 +37,8 @@ def calls_command(out: str) -> list:
     """Compiles the extension module over libtl; libtl is found beside it."""
     import torch
     home = os.path.dirname(torch.__file__)
-    rocm = os.path.dirname(os.path.dirname(HIPCC))
+    # HIPCC may be a name that PATH finds, or a link into the installation
+    rocm = os.path.dirname(os.path.dirname(os.path.realpath(shutil.which(HIPCC) or HIPCC)))
     return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__=1",
             "-DUSE_ROCM=1", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
             "-isystem", os.path.join(home, "include"), "-isystem", os.path.join(rocm, "include"),
