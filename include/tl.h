@@ -676,9 +676,11 @@ int tl_kv_keep(const tl_kv_cache* cache, const int32_t* page_table, int64_t max_
  * bytes, the rest 4), negative counts, max_pages < 1, q_heads not a positive
  * multiple of kv_heads, a bad ldq (see tl_kv_append) or scale, mask_words < 1
  * with a mask, or O overlapping an input; TL_EUNSUPPORTED for max_len or
- * total_q * q_heads above 2^30, mask_words above 2^16, ldq above 2^30 or
- * 2^24 workgroups or more (a tile of 16 to 128 rows each); TL_ENOMEM if the
- * workspace cannot be allocated.  total_q == 0 or num_seqs == 0 enqueues nothing.
+ * total_q * q_heads above 2^30, mask_words above 2^16, ldq above 2^30, a scale
+ * whose product with log2(e) overflows fp32 (above 2.35e38), or 2^24
+ * workgroups or more (a tile of 16 to 128 rows each); TL_ENOMEM if the
+ * workspace cannot be allocated.  total_q == 0 or num_seqs == 0 enqueues
+ * nothing.
  */
 int tl_attn(const void* Q, int64_t ldq, const tl_kv_cache* cache, const int32_t* page_table, int64_t max_pages,
             const int32_t* lens, const int32_t* q_offsets, const uint32_t* mask, int32_t mask_words,

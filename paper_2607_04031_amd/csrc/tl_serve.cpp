@@ -12,6 +12,7 @@ namespace {
 constexpr int64_t kMaxInt = 0x7fffffff;
 constexpr int64_t kMaxStride = int64_t(1) << 30;
 constexpr int kMaxNodes = 4096;
+constexpr float kLog2e = 1.44269504088896340736f;
 
 bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 bool bad_pointer(const void* p, uintptr_t to) { return !p || !aligned(p, to); }
@@ -219,6 +220,7 @@ int tl_attn(const void* Q, int64_t ldq, const tl_kv_cache* cache, const int32_t*
         if (bad_pointer(Q, 16) || bad_pointer(O, 16) || bad_pointer(page_table, 4) || bad_pointer(lens, 4) || bad_pointer(q_offsets, 4)) return TL_EINVAL;
         if (ldq < width || ldq % 8) return TL_EINVAL;
     }
+    if (!std::isfinite(scale * kLog2e)) return TL_EUNSUPPORTED;
     if (ldq > kMaxStride || max_len > kMaxStride || q_heads > kMaxStride / std::max<int64_t>(total_q, 1) || (mask && mask_words > 65536)) return TL_EUNSUPPORTED;
     if (total_q == 0 || num_seqs == 0 || max_q == 0) return TL_OK;
     if (max_pages > kMaxInt) return TL_EUNSUPPORTED;
@@ -239,7 +241,7 @@ int tl_attn(const void* Q, int64_t ldq, const tl_kv_cache* cache, const int32_t*
     a.max_q = std::min(max_q, total_q);
     a.max_len = max_len;
     a.q_heads = q_heads;
-    a.scale_log2 = scale * 1.44269504088896340736f;
+    a.scale_log2 = scale * kLog2e;
     a.out = static_cast<uint16_t*>(O);
     const int64_t floats = plan_attn(&a, D, cache->elem_bytes);
     if (a.max_tiles > most_workgroups(kAttnThreads)) return TL_EUNSUPPORTED;

@@ -36,3 +36,11 @@ def test_verify():
         tl.tl_verify(**d)
     assert status(verify, total_nodes=1 << 24) == tl.TL_EUNSUPPORTED
     assert status(verify, num_seqs=1 << 22) == tl.TL_EUNSUPPORTED
+
+
+def test_attn_scale():
+    """The kernels take scores in units of log2(e): a scale that overflows there has no finite scores."""
+    for scale in (2.36e38, 3.4e38):
+        assert status(tl.tl_attn, Q=addr(4), ldq=64 * 128, cache=cache(), page_table=addr(7), max_pages=4, lens=addr(8), q_offsets=addr(9),
+                      mask=None, mask_words=0, num_seqs=3, total_q=12, max_q=6, max_len=200, q_heads=64, scale=scale, O=addr(11),
+                      stream=0) == tl.TL_EUNSUPPORTED, scale
