@@ -13,10 +13,12 @@
 // the lane, and the page layout has both operands lie as 16-byte chunks in
 // lane order.  8-bit entries become bf16 in registers: keys with their scale
 // (a power of two: exact), values without it, the probabilities times the
-// values' scale being rounded to bf16 in any case.
+// values' scale being rounded to bf16 in any case: the operand holds no more.
+// The sum l is of the unrounded ones.  Against 64 bits the error is 2.2e-3 of
+// the result, of which the output's own rounding is 1.7e-3.
 //
 // Single tokens are bound by HBM: 32 sequences of up to 8192 tokens, 64 heads
-// over 8, 8 bits: 58 us, 5.8 TB/s, and 4.7 us for the join.  Few chunks per
+// over 8, 8 bits: 59 us, 5.7 TB/s, and 4.8 us for the join.  Few chunks per
 // workgroup are bound by its start and end: three chains of five tokens over
 // 131072, 8 heads over one, 30 us (2.5 TB/s) and 7 us; one token over 517, 7 us.
 #include <hip/hip_runtime.h>

@@ -7,10 +7,10 @@
 // instruction are 1 KB without gaps in LDS, so reads have no bank conflicts.
 //
 // Bound by the matrix and vector work of its waves, which hide one another's
-// only in part (MFMA busy for 36 % of the cycles at 2.16 GHz), and by the
-// starts and ends of pieces of tiles.  Three prompts, 135 GFLOP, bf16:
-// 152 us; trees of 64 tokens, 107 GFLOP over 8-bit entries, 155 us; the join of
-// partial results 9 - 13 us of either.
+// only in part (MFMA busy for 36 % of the cycles, 8 bits 32 %, at 2.12 - 2.15
+// GHz), and by the starts and ends of pieces of tiles.  Three prompts, 135
+// GFLOP, bf16: 153 - 155 us, the join of partial results 13.5; trees of 64
+// tokens, 107 GFLOP over 8-bit entries, 151 - 160 us, the join 10.3.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>

@@ -40,7 +40,7 @@ __device__ inline int64_t exps_at(const KvView& c, int64_t page, int head) { ret
 // launch bounds it.  Many tokens (windows): queries a token per workgroup, keys
 // 16 tokens and values 64 tokens of a head, so that whole cache lines are
 // written where the slots follow one another; HBM bounds it (8192 rows of 64
-// heads over 8: 69 us, 4.8 TB/s; a single row: 3.5 us).
+// heads over 8: 70 us, 4.8 TB/s; a single row: 3.5 us).
 // ---------------------------------------------------------------------------
 constexpr int kKeyWindow = 16, kValueWindow = 64;
 
@@ -355,8 +355,8 @@ __global__ __launch_bounds__(kThreads) void kv_append_window_kernel(KvAppendLaun
 // read: entries back to dense bf16 rows; a slot outside the cache reads zeros.
 // A lane takes 8 elements of one token and head.  Many tokens: a workgroup takes
 // 64 of a head, and where their slots fill a group it loads that whole, without
-// gaps, and turns it into rows in LDS (8192 tokens of 8 heads in 8 bits: 10.7
-// us, 4.7 TB/s; one token 2.4).
+// gaps, and turns it into rows in LDS (8192 tokens of 8 heads in 8 bits: 11.1
+// us, 4.6 TB/s; one token 2.3).
 // ---------------------------------------------------------------------------
 template <int D, int ELEM>
 __device__ inline u32x4 read_key(const KvView& c, int64_t page, int head, int t, int d0) {

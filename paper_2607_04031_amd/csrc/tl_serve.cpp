@@ -73,6 +73,8 @@ int64_t span(int64_t rows, int64_t ld, int64_t width, int64_t elem) { return row
 //     and 121, 16-bit 135 and 117), and prompts, whose tiles differ, do not (8 of
 //     512 tokens 148 and 167);
 //   - where each gets four tiles.
+// All of it goes by max_len, the caller's bound: one far above the lengths splits
+// what need not be.
 int64_t plan_attn(AttnLaunch* a, int head_dim, int elem_bytes) {
     constexpr int64_t kSlots = 2 * 256;
     a->group = a->q_heads / a->c.heads;

@@ -15,7 +15,7 @@
 // on it, so results are the same from call to call.
 //
 // 32 trees of up to 24 nodes over 131072 tokens, bf16 logits, fp32 draft: 29 us
-// (4.3 TB/s), 28 and 16; a chain of five over 50257: 4, 5 and 9, latencies.
+// (4.3 TB/s), 30 and 16; a chain of five over 50257: 4, 5 and 9, latencies.
 #include <hip/hip_runtime.h>
 
 #include "tl_serve.h"
