@@ -589,7 +589,8 @@ enum { TL_IN_F32 = 0, TL_IN_BF16 = 1 };
  * rounded once, to nearest even.  E4M3: a token's head is stored with the
  * smallest exponent e with max |x| <= 448 * 2^e, -126 <= e; scaling by 2^-e is
  * exact (values below 2^-126 aside).  Infinities are stored as the largest
- * value, NaNs as NaN (they do not count for the maximum).
+ * value, 448 * 2^120 (which is past bf16 and fp32, and reads as infinity), NaNs
+ * as NaN (they do not count for the maximum).
  * Errors: TL_EINVAL for a bad cache (see tl_kv_bytes), NULL or misaligned
  * pointers (slots, positions, inv_freq 4-byte aligned), n < 0, negative
  * q_heads, a row stride below a row's length or not a multiple of 16 bytes, a
