@@ -536,7 +536,17 @@ int tl_gemm_noalloc(const void* A, const void* W, void* C, int64_t M, int64_t N,
  *   v_exp  [page][head][t / 64][t % 16 / 4][t % 64 / 16][t % 4]
  * All of it 16-byte aligned.  Nothing needs to be initialised: a slot is read
  * only once a token was written to it.
+ * 4 bits (elem_bytes TL_KV_E2M1): OCP E2M1 (+-0, 0.5, 1, 1.5, 2, 3, 4, 6) times
+ * 2^(x - 127), x one byte per token, head and block of 32 elements, b = d / 32 of
+ * B = head_dim / 32 (OCP's microscaling format MXFP4); 255 makes its block NaN.
+ * A page holds page_tokens * head_dim / 2 bytes per head in k, and in v; a byte
+ * holds two elements, the first one low: keys d and d + 1, values d and d + 16.
+ *   k      [page][head][t / 16][b][t % 16][d % 32 / 2]
+ *   v      [page][head][t / 64][b][t % 16 / 4][d % 16][t % 64 / 16][t % 4]
+ *   k_exp  [page][head][t / 64][b][t % 16][t % 64 / 16]
+ *   v_exp  [page][head][t / 64][b][t % 16 / 4][t % 64 / 16][t % 4]
  */
+enum { TL_KV_E2M1 = -4 };    /* elem_bytes of 4-bit elements: minus their bits */
 typedef struct tl_kv_cache {
     void* k;
     void* v;
@@ -546,7 +556,7 @@ typedef struct tl_kv_cache {
     int32_t page_tokens;   /* a power of two, 64 .. 4096 */
     int32_t kv_heads;      /* 1 .. 1024 */
     int32_t head_dim;      /* 64 or 128 */
-    int32_t elem_bytes;    /* 1 (E4M3) or 2 (bf16) */
+    int32_t elem_bytes;    /* 1 (E4M3), 2 (bf16) or TL_KV_E2M1 */
 } tl_kv_cache;
 
 /* tl_kv_bytes -- host only: bytes of k (and of v) into *data, of k_exp (and
@@ -590,7 +600,9 @@ enum { TL_IN_F32 = 0, TL_IN_BF16 = 1 };
  * smallest exponent e with max |x| <= 448 * 2^e, -126 <= e; scaling by 2^-e is
  * exact (values below 2^-126 aside).  Infinities are stored as the largest
  * value, 448 * 2^120 (which is past bf16 and fp32, and reads as infinity), NaNs
- * as NaN (they do not count for the maximum).
+ * as NaN (they do not count for the maximum).  E2M1: the same per block of 32
+ * elements, with max |x| <= 6 * 2^e, -126 <= e <= 125: what is larger than 6 *
+ * 2^125, infinities too, is stored as that, and a NaN makes its block NaN.
  * Errors: TL_EINVAL for a bad cache (see tl_kv_bytes), NULL or misaligned
  * pointers (slots, positions, inv_freq 4-byte aligned), n < 0, negative
  * q_heads, a row stride below a row's length or not a multiple of 16 bytes, a
@@ -608,7 +620,8 @@ int tl_kv_append(const void* Q, int64_t ldq, const void* K, int64_t ldk, const v
  * tl_kv_read -- entries back as values: K_out[i], V_out[i] = the entry at
  * slots[i], bf16 [n][kv_heads][head_dim] (exact: a stored value has at most
  * eight significant bits; E4M3 values times 2^-126 or less may round to
- * subnormal bf16).  A slot outside the cache reads zeros.  Either output may
+ * subnormal bf16; a block of E2M1 that was written otherwise, with a scale above
+ * 2^125, reads infinities where its values are past bf16).  A slot outside the cache reads zeros.  Either output may
  * be NULL.  Errors: TL_EINVAL for a bad cache, NULL or misaligned pointers,
  * n < 0, both outputs NULL, or outputs that overlap the cache, slots or each
  * other; TL_EUNSUPPORTED for 2^24 workgroups or more (64 rows of a head are
@@ -668,10 +681,13 @@ int tl_kv_keep(const tl_kv_cache* cache, const int32_t* page_table, int64_t max_
  * O:          device bf16 [total_q][q_heads][head_dim]; must not overlap the
  *             inputs.
  * Products run on MFMA with bf16 operands and fp32 sums: E4M3 keys times
- * their scale and values are bf16 exactly, the probabilities (times the
- * values' scale) are rounded to bf16; maxima, sums and the output are fp32
- * until it is rounded.  Results are the same from call to call with the same
- * bounds.  Keys of one sequence may be split over workgroups, whose partial
+ * their scale and values are bf16 exactly, E2M1 keys and values times their
+ * scales too, the probabilities (E4M3: times the values' scale) are rounded to
+ * bf16; maxima, sums and the output are fp32
+ * until it is rounded.  The sums are divided by their weights at the end, and
+ * until then up to 2^8 lens[s] times larger: with values of 2^120 / lens[s] and
+ * more they may overflow to infinity.  Results are the same from call to call
+ * with the same bounds.  Keys of one sequence may be split over workgroups, whose partial
  * results take library workspace of the stream (see "HIP graphs" above).
  * Errors: TL_EINVAL for a bad cache, NULL or misaligned pointers (Q and O 16
  * bytes, the rest 4), negative counts, max_pages < 1, q_heads not a positive

@@ -49,6 +49,7 @@ EXPORTED = ("tl_tile_bytes", "tl_repack", "tl_unpack", "tl_gemm", "tl_gemm_noall
             "tl_stream_read", "tl_fetch_counter_read", "tl_release", "tl_strerror")
 TL_VIEW_MAX_RANK = 5
 TL_IN_F32, TL_IN_BF16 = 0, 1
+TL_KV_E2M1 = -4
 
 
 class View(ctypes.Structure):
@@ -125,25 +126,34 @@ class RopeDesc(ctypes.Structure):
 
 class KVCache:
     """tl_kv_cache over tensors that it keeps alive: k and v [pages, kv_heads, page_tokens * head_dim] (uint8 holding
-    E4M3, float8_e4m3fn or bfloat16), k_exp and v_exp uint8 [pages, kv_heads, page_tokens] (None for bfloat16)."""
+    E4M3, float8_e4m3fn or bfloat16), k_exp and v_exp uint8 [pages, kv_heads, page_tokens] (None for bfloat16).  4 bits
+    (float4_e2m1fn_x2, or uint8 with elem_bytes=TL_KV_E2M1): k and v [pages, kv_heads, page_tokens * head_dim / 2], k_exp
+    and v_exp [pages, kv_heads, page_tokens * head_dim / 32]."""
 
-    def __init__(self, k, v, k_exp, v_exp, page_tokens, kv_heads, head_dim):
+    def __init__(self, k, v, k_exp, v_exp, page_tokens, kv_heads, head_dim, elem_bytes=None):
         import torch
-        if any(x.dtype not in (torch.uint8, torch.float8_e4m3fn, torch.bfloat16) for x in (k, v)) or \
-                any(x is not None and x.dtype != torch.uint8 for x in (k_exp, v_exp)):
-            raise ValueError("k and v are uint8 or float8_e4m3fn (E4M3), or bfloat16, exponents uint8")
+        pair = getattr(torch, "float4_e2m1fn_x2", None)
+        if elem_bytes is None and pair is not None and k.dtype == v.dtype == pair:
+            elem_bytes = TL_KV_E2M1
+        if elem_bytes not in (None, TL_KV_E2M1, k.element_size()):
+            raise ValueError("elem_bytes is TL_KV_E2M1, or that of k and v")
+        four = elem_bytes == TL_KV_E2M1
+        types = (torch.uint8, pair or torch.uint8) if four else (torch.uint8, torch.float8_e4m3fn, torch.bfloat16)
+        if any(x.dtype not in types for x in (k, v)) or any(x is not None and x.dtype != torch.uint8 for x in (k_exp, v_exp)):
+            raise ValueError("k and v are uint8 or float8_e4m3fn (E4M3), or bfloat16, or with TL_KV_E2M1 uint8 or "
+                             "float4_e2m1fn_x2, exponents uint8")
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
         self.page_tokens, self.kv_heads, self.head_dim = page_tokens, kv_heads, head_dim
-        self.elem_bytes = k.element_size()
-        block = page_tokens * kv_heads * head_dim
-        self.num_pages = k.numel() // block
-        if k.numel() != self.num_pages * block or v.numel() != k.numel() or v.element_size() != k.element_size():
+        self.elem_bytes = TL_KV_E2M1 if four else k.element_size()
+        block = page_tokens * kv_heads * head_dim // (2 if four else 1)
+        self.num_pages = k.numel() // block if block > 0 else 0
+        if block <= 0 or k.numel() != self.num_pages * block or v.numel() != k.numel() or v.element_size() != k.element_size():
             raise ValueError("k and v must hold whole pages of the same type")
         if (k_exp is None) != (self.elem_bytes == 2) or (v_exp is None) != (self.elem_bytes == 2):
-            raise ValueError("8-bit caches have exponents, and only they")
+            raise ValueError("4- and 8-bit caches have exponents, and only they")
         for x in (k_exp, v_exp):
-            if x is not None and (x.numel() != self.num_pages * page_tokens * kv_heads):
-                raise ValueError("one exponent byte per token and head")
+            if x is not None and (x.numel() != self.num_pages * page_tokens * kv_heads * (head_dim // 32 if four else 1)):
+                raise ValueError("one exponent byte per token and head (4 bits: and 32 elements)")
         self.desc = KVCacheDesc(_ptr(k), _ptr(v), _ptr(k_exp), _ptr(v_exp), self.num_pages, page_tokens, kv_heads,
                                 head_dim, self.elem_bytes)
 
@@ -531,15 +541,17 @@ def gemm(A, W, N, desc: LayoutDesc, fetch_mode=TL_FETCH_BLOCK, out=None, stream=
 
 
 def kv_cache(num_pages, kv_heads, head_dim, page_tokens=64, elem_bytes=1, device="cuda") -> KVCache:
-    """An empty cache: 8-bit (E4M3 with scales) or, with elem_bytes=2, bf16."""
+    """An empty cache: 8-bit (E4M3 with scales) or, with elem_bytes=2, bf16, or, with elem_bytes=TL_KV_E2M1, 4-bit (E2M1
+    with a scale for 32 elements)."""
     import torch
-    dt = torch.uint8 if elem_bytes == 1 else torch.bfloat16
+    dt = torch.bfloat16 if elem_bytes == 2 else torch.uint8
+    four = elem_bytes == TL_KV_E2M1
     data, exps = tl_kv_bytes(KVCacheDesc(None, None, None, None, num_pages, page_tokens, kv_heads, head_dim, elem_bytes))
-    k, v = (torch.empty((num_pages, kv_heads, page_tokens * head_dim), dtype=dt, device=device) for _ in range(2))
+    k, v = (torch.empty((num_pages, kv_heads, page_tokens * head_dim // (2 if four else 1)), dtype=dt, device=device) for _ in range(2))
     assert k.numel() * k.element_size() == data
-    ke, ve = (torch.empty((num_pages, kv_heads, page_tokens), dtype=torch.uint8, device=device) if exps else None
+    ke, ve = (torch.empty((num_pages, kv_heads, exps // (num_pages * kv_heads)), dtype=torch.uint8, device=device) if exps else None
               for _ in range(2))
-    return KVCache(k, v, ke, ve, page_tokens, kv_heads, head_dim)
+    return KVCache(k, v, ke, ve, page_tokens, kv_heads, head_dim, elem_bytes)
 
 
 def rope(positions, inv_freq, sections=None, interleaved=False) -> Rope:

@@ -39,15 +39,17 @@ template <int D, int ELEM, int NT, int RG>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void attn_kernel(AttnLaunch a) {
     constexpr int kRows = 16 * NT * RG;            // of the tile; a wave has 16 NT of them
     constexpr int kKeyWaves = kWaves / RG;         // waves that share rows split the chunks
-    constexpr int kBlocks = 4 / ELEM;              // 16-key blocks of a chunk
+    constexpr bool kFour = kv_four<ELEM>();
+    constexpr int kBlocks = kFour ? 4 : 4 / ELEM;  // 16-key blocks of a chunk
     constexpr int kKeys = 16 * kBlocks;
     constexpr int kParts = NT == 2 && kBlocks == 4 ? 2 : 1;    // of a chunk, one after the other, for registers
-    constexpr int kLoads = D / 16;                 // 1 KB loads of a chunk's keys, and of its values
-    constexpr int kPer = kLoads / kBlocks;         // of a block's keys
+    constexpr int kLoads = kFour ? D / 32 : D / 16;    // 1 KB loads of a chunk's keys, and of its values
+    constexpr int kPer = kFour ? 1 : kLoads / kBlocks; // of a block's keys
+    constexpr int kTokenBytes = kv_width<D, ELEM>() * kv_size<ELEM>();
     constexpr int kSteps = D / 32;                 // MFMA steps along the head
     constexpr int kPad = D + 4;
-    // 32 rows over 8-bit keys: the queries stay in LDS (which holds the results later), for registers
-    constexpr bool kQueriesInLds = NT == 2 && ELEM == 1 && D == 128;
+    // 32 rows over 4- and 8-bit keys: the queries stay in LDS (which holds the results later), for registers
+    constexpr bool kQueriesInLds = NT == 2 && ELEM != 2 && D == 128;
     __shared__ __attribute__((aligned(16))) float o_s[kWaves * 16 * NT * kPad];
     __shared__ float m_s[kKeyWaves][kRows], l_s[kKeyWaves][kRows];
     // rows' elements that an infinity (bit 0), -infinity (1) or NaN (2) among the values reaches: 4 bits each
@@ -84,7 +86,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
             if (!valid) own[nt] = -1;
 #pragma unroll
             for (int f = 0; f < kSteps; ++f) {
-                const int d = ELEM == 1 ? (4 * (f / 2) + g) * 16 + f % 2 * 8 : (4 * f + g) * 8;
+                const int d = kFour ? D / 4 * g + 8 * f : ELEM == 1 ? (4 * (f / 2) + g) * 16 + f % 2 * 8 : (4 * f + g) * 8;
                 const u32x4 x = *reinterpret_cast<const u32x4*>(qp + d);       // rows past the end: the first one's, not stored
                 if (kQueriesInLds) q_s[(nt * kSteps + f) * 64] = x;            // waves that share rows write the same
                 else q[nt][f] = x;
@@ -103,18 +105,32 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
         // Keys of the next chunk are loaded under this one's softmax and second product, its values under the next one's
         // first, page numbers a chunk earlier.  Past the end (and for pages that are none) a block that exists is loaded.
         u32x4 kw[kBlocks][kPer], vw[kLoads], v_exp = {0, 0, 0, 0};
+        AttnKey4<D> kw4[kFour ? kBlocks : 1];
+        u32x4 v_exp4[kFour ? kLoads : 1];
         uint32_t k_exp = 0;
         auto load_keys = [&](int64_t block) {
-            const u32x4* p = reinterpret_cast<const u32x4*>(a.c.k + max(block, int64_t(0)) * (D * ELEM)) + lane;
+            if (kFour) {
+#pragma unroll
+                for (int mb = 0; mb < kBlocks; ++mb)
+                    kw4[kFour ? mb : 0] = attn_key4<D, RG == 1>(a.c.k + (max(block, int64_t(0)) + 16 * mb) * kTokenBytes, lane);
+                k_exp = *reinterpret_cast<const uint32_t*>(a.c.k_exp + max(block, int64_t(0)) * kv_exps<D, ELEM>() + attn_key4_exp<D>(lane));
+                return;
+            }
+            const u32x4* p = reinterpret_cast<const u32x4*>(a.c.k + max(block, int64_t(0)) * kTokenBytes) + lane;
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) kw[i / kPer][i % kPer] = RG == 1 ? __builtin_nontemporal_load(p + i * 64) : p[i * 64];
             if (ELEM == 1) k_exp = *reinterpret_cast<const uint32_t*>(a.c.k_exp + max(block, int64_t(0)) + col * 4);
         };
         auto load_values = [&](int64_t block) {
-            const u32x4* p = reinterpret_cast<const u32x4*>(a.c.v + max(block, int64_t(0)) * (D * ELEM)) + lane;
+            const u32x4* p = reinterpret_cast<const u32x4*>(a.c.v + max(block, int64_t(0)) * kTokenBytes) + lane;
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) vw[i] = RG == 1 ? __builtin_nontemporal_load(p + i * 64) : p[i * 64];
             if (ELEM == 1) v_exp = *reinterpret_cast<const u32x4*>(a.c.v_exp + max(block, int64_t(0)) + g * 16);
+            if (kFour) {
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i)
+                    v_exp4[kFour ? i : 0] = *reinterpret_cast<const u32x4*>(a.c.v_exp + max(block, int64_t(0)) * kv_exps<D, ELEM>() + i * 64 + g * 16);
+            }
         };
         // a 32-key operand of O^T = V^T P^T: half h of an 8-bit load's 16 keys, or a whole 16-bit load
         auto value_of = [&](int db, int h) {
@@ -154,7 +170,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 #pragma unroll
                     for (int mb = 0; mb < kB; ++mb) {
                         u32x4 kf;
-                        if (ELEM == 1) {
+                        if (kFour) {
+                            kf = fp4_to_bf16x8(kw4[kFour ? mb0 + mb : 0].step[f], attn_exp4(k_exp, mb0 + mb));
+                        } else if (ELEM == 1) {
                             const float scale = exp_scale(k_exp >> (8 * (mb0 + mb)) & 0xff);
                             const uint32_t lo = kw[mb0 + mb][f / 2][f % 2 * 2], hi = kw[mb0 + mb][f / 2][f % 2 * 2 + 1];
                             kf = u32x4{fp8_to_bf16<false>(lo, scale), fp8_to_bf16<true>(lo, scale), fp8_to_bf16<false>(hi, scale), fp8_to_bf16<true>(hi, scale)};
@@ -176,7 +194,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
                     }
                     // entries past the end may be anything: their scales and values count as 0.  So do infinities and NaNs
                     // among the others for now: 0 * NaN would reach rows that do not see the key
-                    if (part == 0) {
+                    if (part == 0 && kFour) {       // any code is a finite number, under a finite scale
+#pragma unroll
+                        for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+                            for (int mb = 0; mb < kBlocks; ++mb) v_exp4[kFour ? i : 0][mb] &= attn_first_bytes(left - 16 * mb);
+                    }
+                    if (part == 0 && !kFour) {
 #pragma unroll
                         for (int mb = 0; mb < kBlocks; ++mb) {
                             v_exp[mb] &= attn_first_bytes(left - 16 * mb);
@@ -229,8 +253,31 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 // O^T: elements 16 db + 4 g + i of the head, row col
+                if (kFour) {
 #pragma unroll
-                for (int db = 0; db < D / 16; ++db)
+                    for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+                        for (int h = 0; h < kB / 2; ++h) {
+                            const int m = mb0 + 2 * h;
+                            const u32x4 e = v_exp4[kFour ? i : 0];
+                            u32x4 vf[2];
+                            attn_values4(vw[i][m & 3], vw[i][(m + 1) & 3], e[m & 3], e[(m + 1) & 3], &vf[0], &vf[1]);
+                            if (masked) {
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) {
+                                    const uint32_t bad = attn_odd<2>(vf[j / 4][j % 4]);
+                                    vf[j / 4][j % 4] &= ~bad;
+                                    odd |= bad;
+                                }
+                            }
+#pragma unroll
+                            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt) o[nt][2 * i + j] = mfma_16x16x32(vf[j], p[nt][h], o[nt][2 * i + j]);
+                        }
+                }
+#pragma unroll
+                for (int db = 0; db < (kFour ? 0 : D / 16); ++db)
 #pragma unroll
                     for (int h = 0; h < kB / 2; ++h) {
                         const u32x4 vf = value_of(db, mb0 / 2 + h);
@@ -417,8 +464,7 @@ hipError_t attn_rows(const AttnLaunch& a, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_attn(const AttnLaunch& a, int head_dim, int elem_bytes, hipStream_t stream) {
-    if (head_dim == 64) return elem_bytes == 1 ? attn_rows<64, 1>(a, stream) : attn_rows<64, 2>(a, stream);
-    return elem_bytes == 1 ? attn_rows<128, 1>(a, stream) : attn_rows<128, 2>(a, stream);
+    return kv_as(head_dim, elem_bytes, [&](auto d, auto e) { return attn_rows<d(), e()>(a, stream); });
 }
 
 }  // namespace tl

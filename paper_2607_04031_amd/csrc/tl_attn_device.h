@@ -343,6 +343,53 @@ __device__ inline uint32_t attn_odd(uint32_t w) {
     return ((((w & 0x7fff7fffu) + 0x00800080u) & 0x80008000u) >> 15) * 0xffffu;
 }
 
+// 4-bit entries.  A lane's part of a block of 16 keys: D / 4 elements of key col
+// from D / 4 g on, a dword for each MFMA step along the head; their one scale is
+// a byte of the dword of four blocks' at attn_key4_exp.
+template <int D>
+struct AttnKey4 {
+    uint32_t step[D / 32];
+};
+template <int D, bool ONCE>
+__device__ inline AttnKey4<D> attn_key4(const uint8_t* block, int lane) {
+    const int g = lane >> 4, col = lane & 15;
+    AttnKey4<D> k;
+    if (D == 128) {
+        const u32x4* p = reinterpret_cast<const u32x4*>(block) + lane;
+        const u32x4 w = ONCE ? __builtin_nontemporal_load(p) : *p;
+#pragma unroll
+        for (int f = 0; f < D / 32; ++f) k.step[f] = w[f];
+    } else {
+        const u32x2* p = reinterpret_cast<const u32x2*>(block + (g >> 1) * 256 + col * 16 + (g & 1) * 8);
+        const u32x2 w = ONCE ? __builtin_nontemporal_load(p) : *p;
+#pragma unroll
+        for (int f = 0; f < D / 32; ++f) k.step[f] = w[f & 1];
+    }
+    return k;
+}
+template <int D>
+__device__ inline int attn_key4_exp(int lane) { return (lane >> 4) * D / 128 * 64 + (lane & 15) * 4; }
+
+// The scale of byte i of four, in the exponent's bits; the others, which the
+// conversions do not look at, are what comes along.
+__device__ inline float attn_exp4(uint32_t exps, int i) { return __uint_as_float(i < 3 ? exps << (23 - 8 * i) : exps >> 1); }
+
+// Values of 32 keys: dwords of the keys 16 m + 4 g + i (m = 0, 1) hold elements d
+// and d + 16 of key i in byte i, exps their scales.  Operands of O^T = V^T P^T for
+// the 16 elements of the head from d on, and from d + 16 on.
+__device__ inline void attn_values4(uint32_t w0, uint32_t w1, uint32_t exps0, uint32_t exps1, u32x4* lo, u32x4* hi) {
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+        const uint32_t w = m ? w1 : w0, e = m ? exps1 : exps0;
+        const uint32_t a = fp4_to_bf16<0>(w, attn_exp4(e, 0)), b = fp4_to_bf16<1>(w, attn_exp4(e, 1));
+        const uint32_t c = fp4_to_bf16<2>(w, attn_exp4(e, 2)), d = fp4_to_bf16<3>(w, attn_exp4(e, 3));
+        (*lo)[2 * m] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+        (*lo)[2 * m + 1] = __builtin_amdgcn_perm(d, c, 0x05040100u);
+        (*hi)[2 * m] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+        (*hi)[2 * m + 1] = __builtin_amdgcn_perm(d, c, 0x07060302u);
+    }
+}
+
 // bf16 1 if a bf16 is of a kind: infinity, -infinity, NaN
 __device__ inline uint32_t attn_special(uint32_t x, int kind) {
     return (kind == 0 ? x == 0x7f80u : kind == 1 ? x == 0xff80u : (x & 0x7fffu) > 0x7f80u) ? 0x3f80u : 0u;
@@ -360,8 +407,15 @@ __device__ inline void attn_odd_chunk(const AttnLaunch& a, const AttnPiece& p, i
 #pragma unroll 1
     for (int step = 0; step < 3 * (D / 16) * (MB / 2); ++step) {
         const int kind = step % 3, db = step / 3 % (D / 16), h = step / 3 / (D / 16);
-        constexpr int per = 16 / ELEM * 4 / 32;     // 32-key steps of a load: 2 (8 bits) or 1
-        u32x4 vf = reinterpret_cast<const u32x4*>(a.c.v + block * (D * ELEM))[(h / per * (D / 16) + db) * 64 + lane], is, ones;
+        constexpr int per = kv_four<ELEM>() ? 2 : 16 / ELEM * 4 / 32;       // 32-key steps of a load: 2 (4 and 8 bits) or 1
+        const int load = kv_four<ELEM>() ? db / 2 : h / per * (D / 16) + db;
+        u32x4 vf = reinterpret_cast<const u32x4*>(a.c.v + block * (kv_width<D, ELEM>() * kv_size<ELEM>()))[load * 64 + lane], is, ones;
+        if (kv_four<ELEM>()) {
+            const u32x2 e = *reinterpret_cast<const u32x2*>(a.c.v_exp + block * kv_exps<D, ELEM>() + load * 64 + g * 16 + h * 8);
+            u32x4 lo, hi;
+            attn_values4(h ? vf[2] : vf[0], h ? vf[3] : vf[1], e[0], e[1], &lo, &hi);
+            vf = db & 1 ? hi : lo;
+        }
         if (ELEM == 1) {
             const uint32_t lo = h ? vf[2] : vf[0], hi = h ? vf[3] : vf[1];
             vf = u32x4{fp8_to_bf16<false>(lo, 1.f), fp8_to_bf16<true>(lo, 1.f), fp8_to_bf16<false>(hi, 1.f), fp8_to_bf16<true>(hi, 1.f)};

@@ -51,7 +51,9 @@ template <int D, int ELEM>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void attn_wide_kernel(AttnLaunch a) {
     constexpr int kSteps = D / 32;                 // MFMA steps along the head
     constexpr int kOperands = D / 8;               // of a chunk's keys, and of its values: 1 KB each
-    constexpr int kLoads = D * ELEM / 64;          // 16-byte loads of a thread for a chunk's keys, and for its values
+    constexpr bool kFour = kv_four<ELEM>();
+    constexpr int kLoads = kFour ? 1 : D * ELEM / 64;  // 16-byte loads of a thread for a chunk's keys, and for its values (4 bits: D / 8 bytes)
+    constexpr int kTokenBytes = kv_width<D, ELEM>() * kv_size<ELEM>();
     constexpr int kPad = D + 4;
     __shared__ u32x4 kv_s[2][2][kOperands * 64];   // [buffer][keys, values]; at the end the waves' results
     __shared__ __attribute__((aligned(16))) float scale_s[2][kKeys];    // of the values
@@ -92,7 +94,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
             if (!valid) own[nt] = -1;
 #pragma unroll
             for (int f = 0; f < kSteps; ++f) {
-                const int d = ELEM == 1 ? (4 * (f / 2) + g) * 16 + f % 2 * 8 : (4 * f + g) * 8;
+                const int d = kFour ? D / 4 * g + 8 * f : ELEM == 1 ? (4 * (f / 2) + g) * 16 + f % 2 * 8 : (4 * f + g) * 8;
                 q[nt][f] = *reinterpret_cast<const u32x4*>(qp + d);        // rows past the end: the first one's, not stored
             }
         }
@@ -109,6 +111,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
         const AttnPages pages(a, s.seq, piece.head);
         u32x4 kw[ELEM == 1 ? kLoads : 1], vw[kLoads];
         uint32_t k_exp = 0, v_exp = 0, odd = 0;
+        // 4 bits: a block of 16 keys, and of the values 32 of the head's elements (head size 64: half of the keys) for each wave
+        constexpr int kHalves = D / 64;
+        AttnKey4<D> kw4;
+        uint32_t vw4[2 * kHalves], v_exp4[2 * kHalves];
+        const int value_block = kHalves == 2 ? wave : wave / 2, value_half = kHalves == 2 ? 0 : wave % 2;
         // the operand that load i of this wave's values is: (16 of the head's elements, 32 keys)
         auto value_at = [&](int i) {
             const int at = i * kWaves + wave;
@@ -118,8 +125,24 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
         // ones into registers.
         auto fetch = [&](int64_t block, int buffer) {
             const int64_t from = max(block, int64_t(0));
-            const uint8_t* kb = a.c.k + from * (D * ELEM);
-            const uint8_t* vb = a.c.v + from * (D * ELEM);
+            const uint8_t* kb = a.c.k + from * kTokenBytes;
+            const uint8_t* vb = a.c.v + from * kTokenBytes;
+            if (kFour) {
+                kw4 = attn_key4<D, false>(kb + wave * 16 * kTokenBytes, lane);
+                k_exp = *reinterpret_cast<const uint32_t*>(a.c.k_exp + from * kv_exps<D, ELEM>() + attn_key4_exp<D>(lane));
+                const uint32_t* v = reinterpret_cast<const uint32_t*>(vb + value_block * 1024 + lane * 16) + 2 * value_half;
+                const uint32_t* e = reinterpret_cast<const uint32_t*>(a.c.v_exp + from * kv_exps<D, ELEM>() + value_block * 64 + g * 16) + 2 * value_half;
+                if (kHalves == 2) {
+                    const u32x4 x = *reinterpret_cast<const u32x4*>(v), y = *reinterpret_cast<const u32x4*>(e);
+#pragma unroll
+                    for (int m = 0; m < 2 * kHalves; ++m) vw4[m] = x[m], v_exp4[m] = y[m];
+                } else {
+                    const u32x2 x = *reinterpret_cast<const u32x2*>(v), y = *reinterpret_cast<const u32x2*>(e);
+#pragma unroll
+                    for (int m = 0; m < 2 * kHalves; ++m) vw4[m] = x[m & 1], v_exp4[m] = y[m & 1];
+                }
+                return;
+            }
             if (ELEM == 2) {
 #pragma unroll
                 for (int i = 0; i < kLoads; ++i) {
@@ -145,6 +168,31 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
             u32x4* ks = kv_s[buffer][0] + lane;
             u32x4* vs = kv_s[buffer][1] + lane;
             const bool masked = decltype(may_mask)::value && chunk * kKeys + kKeys > all_here;
+            if (kFour) {
+                const float scale = attn_exp4(k_exp >> (8 * wave), 0);
+#pragma unroll
+                for (int f = 0; f < kSteps; ++f) ks[(wave * kSteps + f) * 64] = fp4_to_bf16x8(kw4.step[f], scale);
+                if (masked) {           // any code is a finite number, under a finite scale
+#pragma unroll
+                    for (int m = 0; m < 2 * kHalves; ++m) v_exp4[m] &= attn_first_bytes(s.len - chunk * kKeys - 4 * g - 16 * (2 * value_half + m));
+                }
+#pragma unroll
+                for (int h = 0; h < kHalves; ++h) {
+                    u32x4 vf[2];
+                    attn_values4(vw4[2 * h], vw4[2 * h + 1], v_exp4[2 * h], v_exp4[2 * h + 1], &vf[0], &vf[1]);
+                    if (masked) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const uint32_t bad = attn_odd<2>(vf[j / 4][j % 4]);
+                            vf[j / 4][j % 4] &= ~bad;
+                            odd |= bad;
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) vs[((2 * value_block + j) * 2 + value_half + h) * 64] = vf[j];
+                }
+                return;
+            }
             if (masked) {
                 const int left = s.len - chunk * kKeys;             // keys of the chunk that exist
                 if (thread >= left) v_exp = 0;
@@ -280,9 +328,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
             __builtin_amdgcn_sched_barrier(0);
         };
 
-        // 8-bit chunks go from the pages to registers during the chunk but one before theirs, and on into LDS at the start of
+        // 4- and 8-bit chunks go from the pages to registers during the chunk but one before theirs, and on into LDS at the start of
         // the one before; 16-bit ones into LDS during the one before.
-        constexpr int kAhead = ELEM == 1 ? 2 : 1;
+        constexpr bool kInRegisters = ELEM != 2;
+        constexpr int kAhead = kInRegisters ? 2 : 1;
         int64_t block = pages.block(piece.chunk0, pages.page(piece.chunk0, chunk_end));
         int64_t next = pages.block(piece.chunk0 + 1, pages.page(piece.chunk0 + 1, chunk_end));
         int next_page = pages.page(piece.chunk0 + 2, chunk_end);
@@ -290,7 +339,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
             fetch(block, 0);
             if (ELEM == 2) wait_for_lds_loads();
             put(std::true_type(), 0, piece.chunk0);
-            if (ELEM == 1) fetch(next, 0);
+            if (kInRegisters) fetch(next, 0);
         }
         wait_for_lds_loads();
         __syncthreads();
@@ -301,10 +350,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
             for (; chunk < before; ++chunk) {
                 const int buffer = (chunk - piece.chunk0) & 1;
                 const bool more = !kMasked || chunk + 1 < chunk_end;
-                if (ELEM == 1 && more) put(may_mask, buffer ^ 1, chunk + 1);
+                if (kInRegisters && more) put(may_mask, buffer ^ 1, chunk + 1);
                 const int64_t after = pages.block(chunk + 2, next_page);
                 next_page = pages.page(chunk + 3, chunk_end);
-                if (ELEM == 1 || more) fetch(kAhead == 2 ? after : next, buffer ^ 1);
+                if (kInRegisters || more) fetch(kAhead == 2 ? after : next, buffer ^ 1);
                 if (block >= 0 && (!kMasked || chunk < wave_end)) compute(may_mask, buffer, chunk);
                 if (ELEM == 2) {
                     wait_for_lds_loads();
@@ -361,14 +410,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
 }  // namespace
 
 hipError_t launch_attn_wide(const AttnLaunch& a, int head_dim, int elem_bytes, hipStream_t stream) {
-    if (head_dim == 64) {
-        if (elem_bytes == 1) hipLaunchKernelGGL((attn_wide_kernel<64, 1>), dim3(a.groups), dim3(kThreads), 0, stream, a);
-        else hipLaunchKernelGGL((attn_wide_kernel<64, 2>), dim3(a.groups), dim3(kThreads), 0, stream, a);
-    } else {
-        if (elem_bytes == 1) hipLaunchKernelGGL((attn_wide_kernel<128, 1>), dim3(a.groups), dim3(kThreads), 0, stream, a);
-        else hipLaunchKernelGGL((attn_wide_kernel<128, 2>), dim3(a.groups), dim3(kThreads), 0, stream, a);
-    }
-    return hipGetLastError();
+    return kv_as(head_dim, elem_bytes, [&](auto d, auto e) {
+        hipLaunchKernelGGL((attn_wide_kernel<d(), e()>), dim3(a.groups), dim3(kThreads), 0, stream, a);
+        return hipGetLastError();
+    });
 }
 
 }  // namespace tl

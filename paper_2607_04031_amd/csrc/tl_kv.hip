@@ -23,9 +23,10 @@ __device__ inline int64_t page_of(const KvView& c, int slot, int* t) {
 // Byte offset of a (page, head) block, and of its exponents.
 template <int D, int ELEM>
 __device__ inline int64_t block_at(const KvView& c, int64_t page, int head) {
-    return ((page * c.heads + head) << c.log2_page) * (D * ELEM);
+    return ((page * c.heads + head) << c.log2_page) * (kv_width<D, ELEM>() * kv_size<ELEM>());
 }
-__device__ inline int64_t exps_at(const KvView& c, int64_t page, int head) { return (page * c.heads + head) << c.log2_page; }
+template <int D, int ELEM>
+__device__ inline int64_t exps_at(const KvView& c, int64_t page, int head) { return ((page * c.heads + head) << c.log2_page) * kv_exps<D, ELEM>(); }
 
 // ---------------------------------------------------------------------------
 // append: x -> rotated x (queries and keys) -> bf16, or E4M3 with the scale
@@ -33,7 +34,8 @@ __device__ inline int64_t exps_at(const KvView& c, int64_t page, int head) { ret
 // is exact and each element is rounded once.  A lane holds 8 elements of one
 // head.  The angle position * inv_freq is reduced to a fraction of a turn in 64
 // bits (at position 10^5 its 32-bit product would be off by 0.005), once per
-// pair and token of a workgroup, through LDS.
+// pair and token of a workgroup, through LDS.  E2M1: the same per block of 32
+// elements, four lanes, with max |x| <= 6 * 2^e.
 //
 // Few tokens: a workgroup takes one token and a part of its heads, and its
 // values go out byte by byte to their places in the transposed blocks; the
@@ -171,43 +173,83 @@ __device__ inline u32x2 to_fp8(const float (&x)[8], int* exponent) {
     return o;
 }
 
+// E2M1 of a block's elements over four lanes, and the exponent of its scale (128: NaN)
+__device__ inline uint32_t to_fp4(const float (&x)[8], int* exponent) {
+    uint32_t bits = 0;      // of the largest magnitude; a NaN's are the largest of all
+#pragma unroll
+    for (int i = 0; i < 8; ++i) bits = max(bits, __float_as_uint(x[i]) & 0x7fffffffu);
+#pragma unroll
+    for (int m = 1; m < 4; m *= 2) bits = max(bits, uint32_t(__shfl_xor(int(bits), m)));
+    // f * 2^(b - 127), 1 <= f < 2: 6 * 2^e = 1.5 * 2^(2 + e) fits it from e = b - 129 on, one more where f > 1.5
+    int e = int(bits >> 23) - 129 + ((bits & 0x7fffffu) > 0x400000u);
+    e = bits ? min(max(e, -126), 125) : 0;
+    const float inv = exp_scale(127 - e);
+    uint32_t o = 0;         // to nearest even, past 6 (infinities) to 6
+    o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, x[0] * inv, x[1] * inv, 1.f, 0);
+    o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, x[2] * inv, x[3] * inv, 1.f, 1);
+    o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, x[4] * inv, x[5] * inv, 1.f, 2);
+    o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, x[6] * inv, x[7] * inv, 1.f, 3);
+    const bool nan = bits > 0x7f800000u;
+    *exponent = nan ? 128 : e;
+    return nan ? 0u : o;
+}
+
+// whether a lane writes an exponent of its head, and of which block
+template <int ELEM>
+__device__ inline bool has_exp(int lane, int* b) {
+    *b = kv_four<ELEM>() ? lane / 4 : 0;
+    return kv_four<ELEM>() ? lane % 4 == 0 : ELEM == 1 && lane == 0;
+}
+
 // keys of a lane into the cache
 template <int D, int ELEM>
 __device__ inline void put_key(const KvView& c, int slot, int head, int lane, const float (&x)[8]) {
-    int t, e = 0;
+    constexpr int W = kv_width<D, ELEM>(), S = kv_size<ELEM>();
+    int t, b, e = 0;
+    const uint32_t o4 = kv_four<ELEM>() ? to_fp4(x, &e) : 0u;
     const u32x2 o8 = ELEM == 1 ? to_fp8<D / 8>(x, &e) : u32x2{0, 0};
     const int64_t page = page_of(c, slot, &t);
     if (page < 0) return;
-    uint8_t* to = c.k + block_at<D, ELEM>(c, page, head) + kv_key_at<D, ELEM>(t, lane * 8) * ELEM;
-    if (ELEM == 2) {
-        *reinterpret_cast<u32x4*>(to) = to_bf16(x);
-    } else {
-        *reinterpret_cast<u32x2*>(to) = o8;
-        if (lane == 0) c.k_exp[exps_at(c, page, head) + kv_key_exp_at(t)] = uint8_t(e + 127);
-    }
+    uint8_t* to = c.k + block_at<D, ELEM>(c, page, head) + kv_key_at<W, S>(t, lane * (W / (D / 8))) * S;
+    if (ELEM == 2) *reinterpret_cast<u32x4*>(to) = to_bf16(x);
+    else if (ELEM == 1) *reinterpret_cast<u32x2*>(to) = o8;
+    else *reinterpret_cast<uint32_t*>(to) = o4;
+    if (has_exp<ELEM>(lane, &b)) c.k_exp[exps_at<D, ELEM>(c, page, head) + kv_key_exp_at(t, b, kv_exps<D, ELEM>())] = uint8_t(e + 127);
 }
 
-// values of a lane (as stored: 4 bf16 pairs, or two words of E4M3 and the exponent), element by element
+// Stored elements of the values that a lane writes, and where the j-th is.  4
+// bits: the even or the odd bytes of those that it shares with the lane two on.
+template <int ELEM>
+constexpr int value_parts() { return kv_four<ELEM>() ? 4 : 8; }
+template <int ELEM>
+__device__ inline int value_place(int lane, int j) { return kv_four<ELEM>() ? lane / 4 * 16 + lane % 2 * 8 + 2 * j + (lane >> 1 & 1) : lane * 8 + j; }
+
+// values of a lane (as stored: 4 bf16 pairs, two words of E4M3 or one of E2M1, and the exponent), element by element
 template <int D, int ELEM>
 __device__ inline void put_value(const KvView& c, int slot, int head, int lane, u32x4 o, int e) {
-    int t;
+    constexpr int W = kv_width<D, ELEM>(), S = kv_size<ELEM>();
+    int t, b;
     const int64_t page = page_of(c, slot, &t);
     if (page < 0) return;
     const int64_t block = block_at<D, ELEM>(c, page, head);
-    if (ELEM == 2) {
-        uint16_t* v = reinterpret_cast<uint16_t*>(c.v + block);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[kv_value_at<D, 2>(t, lane * 8 + i)] = uint16_t(o[i / 2] >> (i % 2 * 16));
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) c.v[block + kv_value_at<D, 1>(t, lane * 8 + i)] = uint8_t(o[i / 4] >> (i % 4 * 8));
-        if (lane == 0) c.v_exp[exps_at(c, page, head) + kv_value_exp_at(t)] = uint8_t(e + 127);
+    for (int i = 0; i < value_parts<ELEM>(); ++i) {
+        const int at = kv_value_at<W, S>(t, value_place<ELEM>(lane, i));
+        if (ELEM == 2) reinterpret_cast<uint16_t*>(c.v + block)[at] = uint16_t(o[i / 2] >> (i % 2 * 16));
+        else c.v[block + at] = uint8_t(o[i / 4] >> (i % 4 * 8));
     }
+    if (has_exp<ELEM>(lane, &b)) c.v_exp[exps_at<D, ELEM>(c, page, head) + kv_value_exp_at(t, b, kv_exps<D, ELEM>())] = uint8_t(e + 127);
 }
 
 template <int D, int ELEM>
 __device__ inline u32x4 stored(const float (&x)[8], int* e) {
     if (ELEM == 2) return to_bf16(x);
+    if (kv_four<ELEM>()) {
+        const uint32_t mine = to_fp4(x, e), other = uint32_t(__shfl_xor(int(mine), 2));
+        const bool second = threadIdx.x & 2;        // the head's lanes begin at a multiple of 8
+        const uint32_t lo = second ? other : mine, hi = second ? mine : other;
+        return u32x4{second ? (lo >> 4 & 0x0f0f0f0fu) | (hi & 0xf0f0f0f0u) : (lo & 0x0f0f0f0fu) | (hi & 0x0f0f0f0fu) << 4, 0, 0, 0};
+    }
     const u32x2 o = to_fp8<D / 8>(x, e);
     return u32x4{o[0], o[1], 0, 0};
 }
@@ -267,8 +309,9 @@ struct AppendBlocks {
 template <int D, int ELEM, bool F32>
 __global__ __launch_bounds__(kThreads) void kv_append_window_kernel(KvAppendLaunch a, AppendBlocks b) {
     constexpr int kLanes = D / 8, kTokens = kThreads / kLanes;
-    constexpr int kStride = kValueWindow * ELEM + 4;           // bytes of an element's tokens in LDS: an odd number of words
-    __shared__ __attribute__((aligned(16))) uint8_t lds[D * kStride > kKeyWindow * D * 4 ? D * kStride : kKeyWindow * D * 4];
+    constexpr int W = kv_width<D, ELEM>(), S = kv_size<ELEM>();
+    constexpr int kStride = kValueWindow * S + 4;              // bytes of an element's tokens in LDS: an odd number of words
+    __shared__ __attribute__((aligned(16))) uint8_t lds[W * kStride > kKeyWindow * D * 4 ? W * kStride : kKeyWindow * D * 4];
     const int lane = threadIdx.x % kLanes, d0 = lane * 8, mine = threadIdx.x / kLanes;
     if (int(blockIdx.x) < b.keys) {                            // 16 tokens' keys of some heads
         float* cos_s = reinterpret_cast<float*>(lds);
@@ -315,29 +358,31 @@ __global__ __launch_bounds__(kThreads) void kv_append_window_kernel(KvAppendLaun
             }
             const int t = w.place + j;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                uint8_t* to = lds + (d0 + i) * kStride + value_byte<ELEM>(t);
-                if (ELEM == 1) *to = uint8_t(o[i / 4] >> (i % 4 * 8));
-                else *reinterpret_cast<uint16_t*>(to) = uint16_t(o[i / 2] >> (i % 2 * 16));
+            for (int i = 0; i < value_parts<ELEM>(); ++i) {
+                uint8_t* to = lds + value_place<ELEM>(lane, i) * kStride + value_byte<S>(t);
+                if (ELEM == 2) *reinterpret_cast<uint16_t*>(to) = uint16_t(o[i / 2] >> (i % 2 * 16));
+                else *to = uint8_t(o[i / 4] >> (i % 4 * 8));
             }
-            if (ELEM == 1 && lane == 0) a.c.v_exp[exps_at(a.c, w.page, head) + w.start + kv_value_exp_at(t)] = uint8_t(e + 127);
+            int b;
+            if (has_exp<ELEM>(lane, &b))
+                a.c.v_exp[exps_at<D, ELEM>(a.c, w.page, head) + kv_value_exp_at(w.start + t, b, kv_exps<D, ELEM>())] = uint8_t(e + 127);
         }
         if (!w.run) return;
         __syncthreads();
-        uint8_t* group = a.c.v + block_at<D, ELEM>(a.c, w.page, head) + w.start * (D * ELEM);
-        for (int u = threadIdx.x; u < D * ELEM * 4; u += kThreads) {    // 16-byte chunks: their element and bytes
+        uint8_t* group = a.c.v + block_at<D, ELEM>(a.c, w.page, head) + w.start * (W * S);
+        for (int u = threadIdx.x; u < W * S * 4; u += kThreads) {       // 16-byte chunks: their element and bytes
             int d, at;
-            value_chunk<D, ELEM>(u, &d, &at);
+            value_chunk<W, S>(u, &d, &at);
             const uint8_t* from = lds + d * kStride + at;
             if (w.count == kValueWindow) {
                 u32x4 x;
                 __builtin_memcpy(&x, __builtin_assume_aligned(from, 4), 16);
                 reinterpret_cast<u32x4*>(group)[u] = x;
             } else {
-                for (int i = 0; i < 16 / ELEM; ++i) {
-                    const int j = value_token<ELEM>(at / ELEM + i) - w.place;
+                for (int i = 0; i < 16 / S; ++i) {
+                    const int j = value_token<S>(at / S + i) - w.place;
                     if (j < 0 || j >= w.count) continue;
-                    if (ELEM == 1) group[u * 16 + i] = from[i];
+                    if (S == 1) group[u * 16 + i] = from[i];
                     else reinterpret_cast<uint16_t*>(group)[u * 8 + i] = reinterpret_cast<const uint16_t*>(from)[i];
                 }
             }
@@ -360,11 +405,21 @@ __global__ __launch_bounds__(kThreads) void kv_append_window_kernel(KvAppendLaun
 // ---------------------------------------------------------------------------
 template <int D, int ELEM>
 __device__ inline u32x4 read_key(const KvView& c, int64_t page, int head, int t, int d0) {
-    const uint8_t* from = c.k + block_at<D, ELEM>(c, page, head) + kv_key_at<D, ELEM>(t, d0) * ELEM;
+    constexpr int W = kv_width<D, ELEM>(), S = kv_size<ELEM>();
+    const uint8_t* from = c.k + block_at<D, ELEM>(c, page, head) + kv_key_at<W, S>(t, d0 * W / D) * S;
     if (ELEM == 2) return *reinterpret_cast<const u32x4*>(from);
-    const float s = exp_scale(c.k_exp[exps_at(c, page, head) + kv_key_exp_at(t)]);
+    const float s = exp_scale(c.k_exp[exps_at<D, ELEM>(c, page, head) + kv_key_exp_at(t, kv_four<ELEM>() ? d0 / 32 : 0, kv_exps<D, ELEM>())]);
+    if (kv_four<ELEM>()) return fp4_to_bf16x8(*reinterpret_cast<const uint32_t*>(from), s);
     const u32x2 w = *reinterpret_cast<const u32x2*>(from);
     return u32x4{fp8_to_bf16<false>(w[0], s), fp8_to_bf16<true>(w[0], s), fp8_to_bf16<false>(w[1], s), fp8_to_bf16<true>(w[1], s)};
+}
+
+// the codes of eight elements from d0 on, of bytes that hold two of them each
+__device__ inline uint32_t value_codes(const uint8_t (&bytes)[8], int d0) {
+    uint32_t w = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w |= uint32_t(bytes[j] >> (d0 >> 2 & 4) & 15) << (4 * j);
+    return w;
 }
 
 template <int D, int ELEM>
@@ -378,7 +433,13 @@ __device__ inline u32x4 read_value(const KvView& c, int64_t page, int head, int 
             o[j] = uint32_t(v[kv_value_at<D, 2>(t, d0 + 2 * j)]) | uint32_t(v[kv_value_at<D, 2>(t, d0 + 2 * j + 1)]) << 16;
         return o;
     }
-    const float s = exp_scale(c.v_exp[exps_at(c, page, head) + kv_value_exp_at(t)]);
+    const float s = exp_scale(c.v_exp[exps_at<D, ELEM>(c, page, head) + kv_value_exp_at(t, kv_four<ELEM>() ? d0 / 32 : 0, kv_exps<D, ELEM>())]);
+    if (kv_four<ELEM>()) {
+        uint8_t bytes[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) bytes[j] = c.v[block + kv_value_at<D / 2, 1>(t, d0 / 32 * 16 + d0 % 16 + j)];
+        return fp4_to_bf16x8(value_codes(bytes, d0), s);
+    }
     u32x2 w = {0, 0};
 #pragma unroll
     for (int j = 0; j < 8; ++j) w[j / 4] |= uint32_t(c.v[block + kv_value_at<D, 1>(t, d0 + j)]) << (j % 4 * 8);
@@ -402,11 +463,12 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(KvView c, const int32
 
 template <int D, int ELEM>
 __global__ __launch_bounds__(kThreads) void kv_read_window_kernel(KvView c, const int32_t* slots, int64_t n, uint16_t* k_out, uint16_t* v_out) {
-    constexpr int kLanes = D / 8, kTokens = kThreads / kLanes, kChunk = 16 / ELEM;
-    constexpr int kRow = D * ELEM + 16;                        // bytes of a token's keys in LDS
-    constexpr int kStride = kValueWindow * ELEM + 4;           // bytes of an element's tokens in LDS
+    constexpr int W = kv_width<D, ELEM>(), S = kv_size<ELEM>();
+    constexpr int kLanes = D / 8, kTokens = kThreads / kLanes, kChunk = 16 / S;
+    constexpr int kRow = W * S + 16;                           // bytes of a token's keys in LDS
+    constexpr int kStride = kValueWindow * S + 4;              // bytes of an element's tokens in LDS
     __shared__ __attribute__((aligned(16))) uint8_t k_s[kValueWindow * kRow];
-    __shared__ __attribute__((aligned(16))) uint8_t v_s[D * kStride];
+    __shared__ __attribute__((aligned(16))) uint8_t v_s[W * kStride];
     const int lane = threadIdx.x % kLanes, d0 = lane * 8, mine = threadIdx.x / kLanes;
     const int head = blockIdx.x % c.heads;
     Window w;
@@ -422,30 +484,41 @@ __global__ __launch_bounds__(kThreads) void kv_read_window_kernel(KvView c, cons
         return;
     }
     // the whole group, 16 bytes a lane without gaps, turned into rows in LDS
-    const int64_t block = block_at<D, ELEM>(c, w.page, head) + w.start * (D * ELEM);
-    constexpr int kChunks = D * ELEM * 4 / kThreads;
+    const int64_t block = block_at<D, ELEM>(c, w.page, head) + w.start * (W * S);
+    constexpr int kAll = W * S * 4, kChunks = (kAll + kThreads - 1) / kThreads;
     u32x4 k[kChunks], v[kChunks];
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
+        if (kAll % kThreads && i * kThreads + int(threadIdx.x) >= kAll) break;
         k[i] = reinterpret_cast<const u32x4*>(c.k + block)[i * kThreads + threadIdx.x];
         v[i] = reinterpret_cast<const u32x4*>(c.v + block)[i * kThreads + threadIdx.x];
     }
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
-        const int u = i * kThreads + threadIdx.x, t = u / (16 * (D / kChunk)) * 16 + (u & 15), j = u / 16 % (D / kChunk);
+        const int u = i * kThreads + threadIdx.x, t = u / (16 * (W / kChunk)) * 16 + (u & 15), j = u / 16 % (W / kChunk);
+        if (kAll % kThreads && u >= kAll) break;
         *reinterpret_cast<u32x4*>(k_s + t * kRow + j * 16) = k[i];
         int d, at;
-        value_chunk<D, ELEM>(u, &d, &at);
+        value_chunk<W, S>(u, &d, &at);
 #pragma unroll
         for (int x = 0; x < 4; ++x) *reinterpret_cast<uint32_t*>(v_s + d * kStride + at + 4 * x) = v[i][x];
     }
     __syncthreads();
     for (int j = mine; j < w.count; j += kTokens) {
         const int t = w.place + j;
-        const int64_t at = ((w.first + j) * c.heads + head) * D + d0, exps = exps_at(c, w.page, head) + w.start;
+        const int64_t at = ((w.first + j) * c.heads + head) * D + d0, exps = exps_at<D, ELEM>(c, w.page, head);
+        constexpr int B = kv_exps<D, ELEM>();
+        const int b = kv_four<ELEM>() ? d0 / 32 : 0;
         u32x4 x;
-        const uint8_t* from = v_s + d0 * kStride + value_byte<ELEM>(t);
-        if (ELEM == 2) {
+        const uint8_t* from = v_s + (kv_four<ELEM>() ? d0 / 32 * 16 + d0 % 16 : d0) * kStride + value_byte<S>(t);
+        if (kv_four<ELEM>()) {
+            x = fp4_to_bf16x8(*reinterpret_cast<const uint32_t*>(k_s + t * kRow + d0 / 2), exp_scale(c.k_exp[exps + kv_key_exp_at(w.start + t, b, B)]));
+            if (k_out) *reinterpret_cast<u32x4*>(k_out + at) = x;
+            uint8_t bytes[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) bytes[i] = from[i * kStride];
+            x = fp4_to_bf16x8(value_codes(bytes, d0), exp_scale(c.v_exp[exps + kv_value_exp_at(w.start + t, b, B)]));
+        } else if (ELEM == 2) {
             x = *reinterpret_cast<const u32x4*>(k_s + t * kRow + d0 * 2);
             if (k_out) *reinterpret_cast<u32x4*>(k_out + at) = x;
 #pragma unroll
@@ -454,13 +527,13 @@ __global__ __launch_bounds__(kThreads) void kv_read_window_kernel(KvView c, cons
                        uint32_t(*reinterpret_cast<const uint16_t*>(from + (2 * i + 1) * kStride)) << 16;
         } else {
             u32x2 y = *reinterpret_cast<const u32x2*>(k_s + t * kRow + d0);
-            float s = exp_scale(c.k_exp[exps + kv_key_exp_at(t)]);
+            float s = exp_scale(c.k_exp[exps + kv_key_exp_at(w.start + t)]);
             x = u32x4{fp8_to_bf16<false>(y[0], s), fp8_to_bf16<true>(y[0], s), fp8_to_bf16<false>(y[1], s), fp8_to_bf16<true>(y[1], s)};
             if (k_out) *reinterpret_cast<u32x4*>(k_out + at) = x;
             y = u32x2{0, 0};
 #pragma unroll
             for (int i = 0; i < 8; ++i) y[i / 4] |= uint32_t(from[i * kStride]) << (i % 4 * 8);
-            s = exp_scale(c.v_exp[exps + kv_value_exp_at(t)]);
+            s = exp_scale(c.v_exp[exps + kv_value_exp_at(w.start + t)]);
             x = u32x4{fp8_to_bf16<false>(y[0], s), fp8_to_bf16<true>(y[0], s), fp8_to_bf16<false>(y[1], s), fp8_to_bf16<true>(y[1], s)};
         }
         if (v_out) *reinterpret_cast<u32x4*>(v_out + at) = x;
@@ -476,10 +549,11 @@ __global__ __launch_bounds__(kThreads) void kv_read_window_kernel(KvView c, cons
 // ---------------------------------------------------------------------------
 template <int D, int ELEM>
 __global__ __launch_bounds__(kThreads) void kv_keep_kernel(KvKeepLaunch a) {
-    constexpr int kBatch = kThreads * 16 / (D * ELEM);      // entries whose keys are one 16-byte chunk per thread
-    constexpr int kElems = kBatch * D / kThreads;           // elements of their values per thread
-    constexpr int kChunks = D * ELEM / 16;
-    using E = typename std::conditional<ELEM == 1, uint8_t, uint16_t>::type;
+    constexpr int W = kv_width<D, ELEM>(), S = kv_size<ELEM>(), B = kv_exps<D, ELEM>();
+    constexpr int kBatch = kThreads * 16 / (W * S);         // entries whose keys are one 16-byte chunk per thread
+    constexpr int kElems = kBatch * W / kThreads;           // stored elements of their values per thread
+    constexpr int kChunks = W * S / 16;
+    using E = typename std::conditional<S == 1, uint8_t, uint16_t>::type;
     __shared__ int page_s[2][kBatch], place_s[2][kBatch];   // of an entry's source and destination; page -1: it stays
     const int seq = blockIdx.x / a.c.heads, head = blockIdx.x - seq * a.c.heads;
     const int32_t* table = a.page_table + int64_t(seq) * a.max_pages;
@@ -509,39 +583,45 @@ __global__ __launch_bounds__(kThreads) void kv_keep_kernel(KvKeepLaunch a) {
         }
         __syncthreads();
         auto key = [&](int end) {                           // of this thread: 0 the source's chunk, 1 the destination's
-            const int i = threadIdx.x / kChunks, d = threadIdx.x % kChunks * (16 / ELEM);
-            return reinterpret_cast<u32x4*>(a.c.k + block_at<D, ELEM>(a.c, page_s[end][i], head) + kv_key_at<D, ELEM>(place_s[end][i], d) * ELEM);
+            const int i = threadIdx.x / kChunks, d = threadIdx.x % kChunks * (16 / S);
+            return reinterpret_cast<u32x4*>(a.c.k + block_at<D, ELEM>(a.c, page_s[end][i], head) + kv_key_at<W, S>(place_s[end][i], d) * S);
         };
         auto value = [&](int end, int u) {
-            return reinterpret_cast<E*>(a.c.v + block_at<D, ELEM>(a.c, page_s[end][u / D], head)) + kv_value_at<D, ELEM>(place_s[end][u / D], u % D);
+            return reinterpret_cast<E*>(a.c.v + block_at<D, ELEM>(a.c, page_s[end][u / W], head)) + kv_value_at<W, S>(place_s[end][u / W], u % W);
         };
         const bool has_key = int(threadIdx.x / kChunks) < some && page_s[0][threadIdx.x / kChunks] >= 0;
-        const bool has_exp = ELEM == 1 && int(threadIdx.x) < some && page_s[0][threadIdx.x] >= 0;
+        const bool has_exps = B && int(threadIdx.x) < some && page_s[0][threadIdx.x] >= 0;
         u32x4 k;
         E v[kElems];
-        uint8_t exps[2];
+        uint8_t exps[2][B ? B : 1];
         if (has_key) k = *key(0);
 #pragma unroll
         for (int j = 0; j < kElems; ++j) {
             const int u = j * kThreads + threadIdx.x;
-            if (u / D < some && page_s[0][u / D] >= 0) v[j] = *value(0, u);
+            if (u / W < some && page_s[0][u / W] >= 0) v[j] = *value(0, u);
         }
-        if (has_exp) {
-            const int64_t at = exps_at(a.c, page_s[0][threadIdx.x], head);
-            exps[0] = a.c.k_exp[at + kv_key_exp_at(place_s[0][threadIdx.x])];
-            exps[1] = a.c.v_exp[at + kv_value_exp_at(place_s[0][threadIdx.x])];
+        if (has_exps) {
+            const int64_t at = exps_at<D, ELEM>(a.c, page_s[0][threadIdx.x], head);
+#pragma unroll
+            for (int b = 0; b < B; ++b) {
+                exps[0][b] = a.c.k_exp[at + kv_key_exp_at(place_s[0][threadIdx.x], b, B)];
+                exps[1][b] = a.c.v_exp[at + kv_value_exp_at(place_s[0][threadIdx.x], b, B)];
+            }
         }
         __syncthreads();
         if (has_key) *key(1) = k;
 #pragma unroll
         for (int j = 0; j < kElems; ++j) {
             const int u = j * kThreads + threadIdx.x;
-            if (u / D < some && page_s[0][u / D] >= 0) *value(1, u) = v[j];
+            if (u / W < some && page_s[0][u / W] >= 0) *value(1, u) = v[j];
         }
-        if (has_exp) {
-            const int64_t at = exps_at(a.c, page_s[1][threadIdx.x], head);
-            a.c.k_exp[at + kv_key_exp_at(place_s[1][threadIdx.x])] = exps[0];
-            a.c.v_exp[at + kv_value_exp_at(place_s[1][threadIdx.x])] = exps[1];
+        if (has_exps) {
+            const int64_t at = exps_at<D, ELEM>(a.c, page_s[1][threadIdx.x], head);
+#pragma unroll
+            for (int b = 0; b < B; ++b) {
+                a.c.k_exp[at + kv_key_exp_at(place_s[1][threadIdx.x], b, B)] = exps[0][b];
+                a.c.v_exp[at + kv_value_exp_at(place_s[1][threadIdx.x], b, B)] = exps[1][b];
+            }
         }
         __syncthreads();
     }
@@ -607,18 +687,15 @@ int64_t kv_read_workgroups(const KvView& c, int head_dim, int64_t n) {
 }
 
 hipError_t launch_kv_append(const KvAppendLaunch& a, int head_dim, int elem_bytes, hipStream_t stream) {
-    if (head_dim == 64) return elem_bytes == 1 ? append_as<64, 1>(a, stream) : append_as<64, 2>(a, stream);
-    return elem_bytes == 1 ? append_as<128, 1>(a, stream) : append_as<128, 2>(a, stream);
+    return kv_as(head_dim, elem_bytes, [&](auto d, auto e) { return append_as<d(), e()>(a, stream); });
 }
 
 hipError_t launch_kv_read(const KvView& c, int head_dim, int elem_bytes, const int32_t* slots, int64_t n, uint16_t* k_out, uint16_t* v_out, hipStream_t stream) {
-    if (head_dim == 64) return elem_bytes == 1 ? read_as<64, 1>(c, slots, n, k_out, v_out, stream) : read_as<64, 2>(c, slots, n, k_out, v_out, stream);
-    return elem_bytes == 1 ? read_as<128, 1>(c, slots, n, k_out, v_out, stream) : read_as<128, 2>(c, slots, n, k_out, v_out, stream);
+    return kv_as(head_dim, elem_bytes, [&](auto d, auto e) { return read_as<d(), e()>(c, slots, n, k_out, v_out, stream); });
 }
 
 hipError_t launch_kv_keep(const KvKeepLaunch& a, int head_dim, int elem_bytes, hipStream_t stream) {
-    if (head_dim == 64) return elem_bytes == 1 ? keep_as<64, 1>(a, stream) : keep_as<64, 2>(a, stream);
-    return elem_bytes == 1 ? keep_as<128, 1>(a, stream) : keep_as<128, 2>(a, stream);
+    return kv_as(head_dim, elem_bytes, [&](auto d, auto e) { return keep_as<d(), e()>(a, stream); });
 }
 
 }  // namespace tl

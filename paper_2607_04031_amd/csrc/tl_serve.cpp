@@ -30,12 +30,13 @@ bool overlap(const Range& a, const Range& b) {
 // The cache's sizes; data and exps: bytes of k (v) and of k_exp (v_exp).
 int check_sizes(const tl_kv_cache* c, int64_t* data, int64_t* exps) {
     if (!c || c->num_pages < 1 || !is_pow2(c->page_tokens) || c->page_tokens < 64 || c->page_tokens > 4096) return TL_EINVAL;
-    if (c->kv_heads < 1 || c->kv_heads > 1024 || (c->elem_bytes != 1 && c->elem_bytes != 2)) return TL_EINVAL;
+    if (c->kv_heads < 1 || c->kv_heads > 1024 || (c->elem_bytes != 1 && c->elem_bytes != 2 && c->elem_bytes != TL_KV_E2M1)) return TL_EINVAL;
     if (c->num_pages > kMaxInt / c->page_tokens) return TL_EINVAL;
     if (c->head_dim != 64 && c->head_dim != 128) return TL_EUNSUPPORTED;
     const int64_t tokens = c->num_pages * c->page_tokens * c->kv_heads;
-    *data = tokens * c->head_dim * c->elem_bytes;
-    *exps = c->elem_bytes == 1 ? tokens : 0;
+    const bool four = c->elem_bytes == TL_KV_E2M1;
+    *data = four ? tokens * c->head_dim / 2 : tokens * c->head_dim * c->elem_bytes;
+    *exps = four ? tokens * c->head_dim / 32 : c->elem_bytes == 1 ? tokens : 0;
     return TL_OK;
 }
 
@@ -43,7 +44,7 @@ int check_cache(const tl_kv_cache* c, int64_t* data, int64_t* exps, KvView* view
     const int rc = check_sizes(c, data, exps);
     if (rc != TL_OK) return rc;
     if (bad_pointer(c->k, 16) || bad_pointer(c->v, 16)) return TL_EINVAL;
-    if (c->elem_bytes == 1 && (bad_pointer(c->k_exp, 16) || bad_pointer(c->v_exp, 16))) return TL_EINVAL;
+    if (*exps && (bad_pointer(c->k_exp, 16) || bad_pointer(c->v_exp, 16))) return TL_EINVAL;
     *view = KvView{static_cast<uint8_t*>(c->k), static_cast<uint8_t*>(c->v), c->k_exp, c->v_exp, c->num_pages,
                    ilog2(c->page_tokens), c->kv_heads};
     return TL_OK;
@@ -83,10 +84,10 @@ int64_t plan_attn(AttnLaunch* a, int head_dim, int elem_bytes) {
     const int64_t group = a->group, most = a->max_q * group;
     a->log2_rows = most <= 16 ? 4 : most <= 32 ? 5 : most <= 64 ? 6 : 7;
     const int64_t rows = int64_t(1) << a->log2_rows;
-    a->log2_keys = elem_bytes == 1 || rows == 128 ? 6 : 5;
+    a->log2_keys = elem_bytes != 2 || rows == 128 ? 6 : 5;
     a->max_tiles = std::min(a->num_seqs * ((most + rows - 1) / rows), a->total_q * group / rows + a->num_seqs) * a->c.heads;
     const bool wide = rows == 128;
-    const int64_t whole = rows > 16 ? 1024 : elem_bytes == 1 ? 2048 : 1536;
+    const int64_t whole = rows > 16 ? 1024 : elem_bytes != 2 ? 2048 : 1536;
     const bool enough = wide ? a->mask && a->max_tiles >= 2 * kSlots && a->max_len <= 2048 : a->max_tiles >= kSlots && a->max_len <= 4096;
     a->split = a->max_len > whole && !enough && a->max_tiles < 4 * kSlots;
     a->groups = int(a->split ? kSlots : a->max_tiles);

@@ -5,6 +5,7 @@
 #pragma once
 
 #include <cstdint>
+#include <type_traits>
 
 #include <hip/hip_runtime.h>
 
@@ -21,6 +22,12 @@ namespace tl {
 // and, 8 bits, the biased exponents of the scales (one per token and head):
 //   keys    [page][head][t / 64][t % 16][t % 64 / 16]
 //   values  [page][head][t / 64][t % 16 / 4][t % 64 / 16][t % 4]
+// 4 bits: bytes as of an 8-bit cache with half the head size, of which byte b
+// holds two elements (keys 2 b and 2 b + 1, values 32 (b / 16) + b % 16 and 16
+// on, the first one low), and of the exponents [B = head size / 32] blocks
+// where 8 bits have one:
+//   keys    [page][head][t / 64][B][t % 16][t % 64 / 16]
+//   values  [page][head][t / 64][B][t % 16 / 4][t % 64 / 16][t % 4]
 struct KvView {
     uint8_t* k;
     uint8_t* v;
@@ -43,8 +50,35 @@ __host__ __device__ inline int kv_value_at(int t, int d) {
     return t / (4 * c) * (4 * c * D) + (d >> 4) * (64 * c) + ((t & 15) >> 2) * (16 * c) + (d & 15) * c +
            (t % (4 * c) >> 4) * 4 + (t & 3);
 }
-__host__ __device__ inline int kv_key_exp_at(int t) { return (t & ~63) + (t & 15) * 4 + ((t & 63) >> 4); }
-__host__ __device__ inline int kv_value_exp_at(int t) { return (t & ~63) + ((t & 15) >> 2) * 16 + ((t & 63) >> 4) * 4 + (t & 3); }
+// Offsets of the exponent of block b of B.
+__host__ __device__ inline int kv_key_exp_at(int t, int b = 0, int B = 1) { return (t & ~63) * B + b * 64 + (t & 15) * 4 + ((t & 63) >> 4); }
+__host__ __device__ inline int kv_value_exp_at(int t, int b = 0, int B = 1) {
+    return (t & ~63) * B + b * 64 + ((t & 15) >> 2) * 16 + ((t & 63) >> 4) * 4 + (t & 3);
+}
+
+// Of an element type (elem_bytes of the cache): the stored elements of a head
+// and their bytes -- of 4 bits, two to a byte -- and the exponents of a token's
+// head.
+template <int ELEM>
+constexpr bool kv_four() { return ELEM == TL_KV_E2M1; }
+template <int D, int ELEM>
+constexpr int kv_width() { return kv_four<ELEM>() ? D / 2 : D; }
+template <int ELEM>
+constexpr int kv_size() { return kv_four<ELEM>() ? 1 : ELEM; }
+template <int D, int ELEM>
+constexpr int kv_exps() { return kv_four<ELEM>() ? D / 32 : ELEM == 1 ? 1 : 0; }
+
+// f(head size, element type) for those of a cache
+template <typename F>
+auto kv_as(int head_dim, int elem_bytes, F f) {
+    using D64 = std::integral_constant<int, 64>;
+    using D128 = std::integral_constant<int, 128>;
+    using E4 = std::integral_constant<int, TL_KV_E2M1>;
+    using E8 = std::integral_constant<int, 1>;
+    using E16 = std::integral_constant<int, 2>;
+    if (head_dim == 64) return elem_bytes == 1 ? f(D64(), E8()) : elem_bytes == 2 ? f(D64(), E16()) : f(D64(), E4());
+    return elem_bytes == 1 ? f(D128(), E8()) : elem_bytes == 2 ? f(D128(), E16()) : f(D128(), E4());
+}
 
 // Workgroups of a launch, at most: HIP takes fewer than 2^32 work-items in a
 // dimension.  The entry points refuse a call with more in any of its launches.

@@ -29,6 +29,18 @@ __device__ inline uint32_t fp8_to_bf16(uint32_t w, float scale) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, HIGH));
 }
 
+// two of a word's eight E2M1 values, of byte BYTE, times a power of two, of which
+// the instruction takes the exponent's bits alone: exact in bf16, infinity past
+// it, NaN if the bits are all ones
+template <int BYTE>
+__device__ inline uint32_t fp4_to_bf16(uint32_t w, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, BYTE));
+}
+// all eight
+__device__ inline u32x4 fp4_to_bf16x8(uint32_t w, float scale) {
+    return u32x4{fp4_to_bf16<0>(w, scale), fp4_to_bf16<1>(w, scale), fp4_to_bf16<2>(w, scale), fp4_to_bf16<3>(w, scale)};
+}
+
 // 2^(e - 127) of a biased exponent
 __device__ inline float exp_scale(uint32_t e) { return __uint_as_float(e << 23); }
 
