@@ -514,8 +514,8 @@ int tl_gemm_noalloc(const void* A, const void* W, void* C, int64_t M, int64_t N,
                     const tl_layout_desc* layout, int32_t fetch_mode, void* stream);
 
 /* ---------------------------------------------------------------------------
- * A serving step around the projections: a paged key/value cache, attention
- * over it, and the verification of drafted tokens.  Of a layer, tl_gemm makes
+ * A serving step around the projections: a paged key/value cache and its pool of
+ * pages, attention over it, and the verification of drafted tokens.  Of a layer, tl_gemm makes
  * the rows of queries, keys and values; tl_kv_append turns and stores them;
  * tl_attn answers; tl_gemm takes its output on.  After the last layer and the
  * head, tl_verify walks every sequence's drafted tokens, and tl_kv_keep moves
@@ -651,6 +651,108 @@ int tl_kv_read(const tl_kv_cache* cache, const int32_t* slots, int64_t n, void* 
  */
 int tl_kv_keep(const tl_kv_cache* cache, const int32_t* page_table, int64_t max_pages, const int32_t* starts,
                const int32_t* path, int64_t max_path, const int32_t* counts, int32_t num_seqs, void* stream);
+
+/*
+ * The pages of a pool: who refers to which.  A pool serves any number of caches
+ * (one per layer) of the same num_pages and page_tokens; row s of the table holds
+ * the pages of sequence s, which tl_kv_keep and tl_attn take as they are.  refs
+ * counts, for every page, the entries of the table that name it (a new pool: all
+ * 0, the table all -1); a page whose count is 0 is free.  The calls below keep it
+ * so, whatever rows they are given, and take the lowest free pages first, in the
+ * order of their lists, so that every call has one result.  Rows and pages
+ * outside the pool are passed over.  All in device memory, without a wait on the
+ * host: a serving loop enqueues them beside its other calls, and they may be
+ * captured (tl_kv_grow, tl_kv_fork and tl_kv_compact take library workspace of the
+ * stream, see "HIP graphs" above).  Calls on one pool must not overlap.
+ */
+typedef struct tl_kv_pages {
+    int32_t* refs;         /* device [num_pages] */
+    int32_t* page_table;   /* device [num_rows][max_pages] */
+    int64_t num_pages;
+    int64_t max_pages;
+    int32_t num_rows;
+    int32_t page_tokens;   /* a power of two, 64 .. 4096 */
+} tl_kv_pages;
+
+/*
+ * tl_kv_grow -- pages for the next tokens: of row rows[i], i < n, every negative
+ * entry among the first ceil(lens[i] / page_tokens) (at most max_pages) gets a
+ * free page, entry after entry, sequence after sequence.
+ *
+ * rows, lens: device int32 [n].
+ * missing:    device int32 [1]: how many entries found no free page (they, and
+ *             only they, stay negative).  Always written.
+ * A row that is named twice gets its pages once, which ones is not specified,
+ * and 'missing' counts it twice.
+ * Errors: TL_EINVAL for NULL or misaligned pointers (4 bytes), sizes below 1, a
+ * bad page_tokens, more than 2^31 - 1 tokens, n < 0, or arrays that overlap;
+ * TL_EUNSUPPORTED for max_pages of 2^31 or more or n above 65536; TL_ENOMEM if
+ * the workspace cannot be allocated.
+ */
+int tl_kv_grow(const tl_kv_pages* pages, const int32_t* rows, const int32_t* lens, int32_t n, int32_t* missing, void* stream);
+
+/*
+ * tl_kv_free -- sequences end, or lose their last tokens: the entries of row
+ * rows[i] from the ceil(lens[i] / page_tokens)-th on (lens NULL: all of them)
+ * become -1, and their pages lose a reference each.  Errors: as tl_kv_grow.
+ * n == 0 enqueues nothing.
+ */
+int tl_kv_free(const tl_kv_pages* pages, const int32_t* rows, const int32_t* lens, int32_t n, void* stream);
+
+/*
+ * tl_kv_fork -- sequences go on in several ways (beams, parallel samples): the
+ * first lens[i] tokens of row parents[i] become those of row children[i].  Full
+ * pages are shared (a reference more); a page that they fill in part is the
+ * child's own, a free one, and a pair of pages to copy (tl_kv_copy, once for
+ * every cache of the pool).  What the child's row held before loses its
+ * references; its other entries become -1.
+ *
+ * parents, children, lens: device int32 [n]; lens are clamped to the table's
+ *             width.
+ * src, dst, tokens: device int32 [n], the pairs in the order of the children:
+ *             the parent's page, the child's, and the tokens in it; then -1.
+ * count:      device int32 [2]: the pairs, and the children for which no page
+ *             was free (their entry stays -1).  Always written.
+ * A row must not be a child twice, nor a child of one and the parent of another:
+ * which tokens it ends up with is not specified then.
+ * Errors: as tl_kv_grow.
+ */
+int tl_kv_fork(const tl_kv_pages* pages, const int32_t* parents, const int32_t* children, const int32_t* lens, int32_t n,
+               int32_t* src, int32_t* dst, int32_t* tokens, int32_t* count, void* stream);
+
+/*
+ * tl_kv_compact -- pages in use move to the front of the pool, whose rest can
+ * then be given up: the k-th page in use from the end goes to the k-th free one
+ * from the front, as long as that comes before it, and k < max_moves (a call
+ * does part of the work).  References and the table follow; what the pages hold
+ * is copied by tl_kv_copy (once for every cache of the pool) before anything
+ * else uses them.
+ *
+ * src, dst:   device int32 [max_moves]: the moves, then -1.
+ * count:      device int32 [2]: the moves, and the pages in use.
+ * Errors: as tl_kv_grow; TL_EINVAL for max_moves < 0, TL_EUNSUPPORTED for 2^31 or
+ * more.
+ */
+int tl_kv_compact(const tl_kv_pages* pages, int64_t max_moves, int32_t* src, int32_t* dst, int32_t* count, void* stream);
+
+/*
+ * tl_kv_copy -- the entries of pages src[i] to pages dst[i], as stored, in a
+ * cache of any element type.
+ *
+ * src, dst:   device int32 [max_pairs]; a pair with a page outside the cache, or
+ *             of one page twice, copies nothing.  No page of dst may be in src
+ *             or twice in dst: what it holds is not specified then.
+ * tokens:     device int32 [max_pairs] or NULL: the first tokens[i] tokens of
+ *             the page, in whole groups of 64 (NULL: all).
+ * count:      device int32 or NULL: pairs from *count on are not looked at
+ *             (tl_kv_fork's and tl_kv_compact's count).
+ * Errors: TL_EINVAL for a bad cache (see tl_kv_bytes), NULL or misaligned
+ * pointers (4 bytes), max_pairs < 0, or lists that overlap the cache's arrays,
+ * or those one another; TL_EUNSUPPORTED for max_pairs of 2^31 or more.
+ * max_pairs == 0 enqueues nothing.
+ */
+int tl_kv_copy(const tl_kv_cache* cache, const int32_t* src, const int32_t* dst, const int32_t* tokens, const int32_t* count,
+               int64_t max_pairs, void* stream);
 
 /*
  * tl_attn -- attention of the new tokens of every sequence over the cache,

@@ -14,6 +14,7 @@ the C names and argument order of ``include/tl.h``:
     tl_gemm_grouped / tl_gemm_grouped_swiglu (..., layout, fetch_mode, stream=None)
     tl_read_amp(M, N, K, tile_m, tile_n, tile_k, layout, G) -> dict
     tl_kv_bytes / tl_kv_append / tl_kv_read / tl_kv_keep (a paged key/value cache)
+    tl_kv_grow / tl_kv_free / tl_kv_fork / tl_kv_compact / tl_kv_copy (its pages)
     tl_attn (attention over it), tl_verify (drafted tokens)
     tl_fetch_counter_read(stream=None) -> int
     tl_release()
@@ -22,7 +23,8 @@ the C names and argument order of ``include/tl.h``:
 Pointer arguments accept a torch CUDA tensor or a raw integer address.
 ``layout`` is a :class:`LayoutDesc` (or a dict of its fields).  A few helpers
 (``repack``, ``gemm``, ``layout``; ``kv_cache``, ``rope``, ``kv_append``,
-``kv_read``, ``kv_keep``, ``attention``, ``verify``) build outputs and
+``kv_read``, ``kv_keep``, ``kv_pages``, ``kv_grow``, ``kv_free``, ``kv_fork``,
+``kv_compact``, ``kv_copy``, ``attention``, ``verify``) build outputs and
 descriptors for callers that just hold tensors.
 
 If libtl.so has not been built the first call raises ``ImportError``; there is
@@ -46,6 +48,7 @@ TL_FETCH_NATIVE, TL_FETCH_BLOCK, TL_FETCH_COUNT = 0, 1, 0x100
 EXPORTED = ("tl_tile_bytes", "tl_repack", "tl_unpack", "tl_gemm", "tl_gemm_noalloc", "tl_gemm_w8", "tl_gemm_plan", "tl_gemm_grouped", "tl_gemm_grouped_swiglu", "tl_read_amp",
             "tl_view_offsets", "tl_view_load", "tl_prefetch_degree", "tl_gemm_lgms", "tl_lgms_occupancy",
             "tl_kv_bytes", "tl_kv_append", "tl_kv_read", "tl_kv_keep", "tl_attn", "tl_verify",
+            "tl_kv_grow", "tl_kv_free", "tl_kv_fork", "tl_kv_compact", "tl_kv_copy",
             "tl_stream_read", "tl_fetch_counter_read", "tl_release", "tl_strerror")
 TL_VIEW_MAX_RANK = 5
 TL_IN_F32, TL_IN_BF16 = 0, 1
@@ -115,6 +118,15 @@ class KVCacheDesc(ctypes.Structure):
                 ("elem_bytes", ctypes.c_int32)]
 
 
+class KVPagesDesc(ctypes.Structure):
+    _fields_ = [("refs", ctypes.c_void_p),
+                ("page_table", ctypes.c_void_p),
+                ("num_pages", ctypes.c_int64),
+                ("max_pages", ctypes.c_int64),
+                ("num_rows", ctypes.c_int32),
+                ("page_tokens", ctypes.c_int32)]
+
+
 class RopeDesc(ctypes.Structure):
     _fields_ = [("positions", ctypes.c_void_p),
                 ("inv_freq", ctypes.c_void_p),
@@ -156,6 +168,17 @@ class KVCache:
                 raise ValueError("one exponent byte per token and head (4 bits: and 32 elements)")
         self.desc = KVCacheDesc(_ptr(k), _ptr(v), _ptr(k_exp), _ptr(v_exp), self.num_pages, page_tokens, kv_heads,
                                 head_dim, self.elem_bytes)
+
+
+class KVPages:
+    """tl_kv_pages over tensors that it keeps alive: refs int32 [pages], table int32 [rows, max_pages]."""
+
+    def __init__(self, refs, table, page_tokens):
+        import torch
+        if refs.dtype != torch.int32 or table.dtype != torch.int32 or refs.dim() != 1 or table.dim() != 2:
+            raise ValueError("refs is int32 [pages], the table int32 [rows, max_pages]")
+        self.refs, self.table, self.page_tokens = refs, table, page_tokens
+        self.desc = KVPagesDesc(_ptr(refs), _ptr(table), refs.numel(), table.shape[1], table.shape[0], page_tokens)
 
 
 class Rope:
@@ -237,6 +260,17 @@ def load_library():
     lib.tl_kv_read.argtypes = [cache, p, i64, p, p, p]
     lib.tl_kv_keep.restype = ctypes.c_int
     lib.tl_kv_keep.argtypes = [cache, p, i64, p, p, i64, p, i32, p]
+    pool = ctypes.POINTER(KVPagesDesc)
+    lib.tl_kv_grow.restype = ctypes.c_int
+    lib.tl_kv_grow.argtypes = [pool, p, p, i32, p, p]
+    lib.tl_kv_free.restype = ctypes.c_int
+    lib.tl_kv_free.argtypes = [pool, p, p, i32, p]
+    lib.tl_kv_fork.restype = ctypes.c_int
+    lib.tl_kv_fork.argtypes = [pool, p, p, p, i32, p, p, p, p, p]
+    lib.tl_kv_compact.restype = ctypes.c_int
+    lib.tl_kv_compact.argtypes = [pool, i64, p, p, p, p]
+    lib.tl_kv_copy.restype = ctypes.c_int
+    lib.tl_kv_copy.argtypes = [cache, p, p, p, p, i64, p]
     lib.tl_attn.restype = ctypes.c_int
     lib.tl_attn.argtypes = [p, i64, cache, p, i64, p, p, p, i32, i32, i64, i64, i64, i32, f32, p, p]
     lib.tl_verify.restype = ctypes.c_int
@@ -454,6 +488,35 @@ def tl_kv_keep(cache, page_table, max_pages, starts, path, max_path, counts, num
                                      _ptr(counts), num_seqs, _stream(stream)), "tl_kv_keep")
 
 
+def _pages_ref(pages):
+    return ctypes.byref(pages.desc if isinstance(pages, KVPages) else pages)
+
+
+def tl_kv_grow(pages, rows, lens, n, missing, stream=None):
+    _check(load_library().tl_kv_grow(_pages_ref(pages), _ptr(rows), _ptr(lens), n, _ptr(missing), _stream(stream)), "tl_kv_grow")
+
+
+def tl_kv_free(pages, rows, lens, n, stream=None):
+    """lens may be None (rows give all their pages back)."""
+    _check(load_library().tl_kv_free(_pages_ref(pages), _ptr(rows), _ptr(lens), n, _stream(stream)), "tl_kv_free")
+
+
+def tl_kv_fork(pages, parents, children, lens, n, src, dst, tokens, count, stream=None):
+    _check(load_library().tl_kv_fork(_pages_ref(pages), _ptr(parents), _ptr(children), _ptr(lens), n, _ptr(src), _ptr(dst),
+                                     _ptr(tokens), _ptr(count), _stream(stream)), "tl_kv_fork")
+
+
+def tl_kv_compact(pages, max_moves, src, dst, count, stream=None):
+    _check(load_library().tl_kv_compact(_pages_ref(pages), max_moves, _ptr(src), _ptr(dst), _ptr(count), _stream(stream)),
+           "tl_kv_compact")
+
+
+def tl_kv_copy(cache, src, dst, tokens, count, max_pairs, stream=None):
+    """tokens and count may be None (whole pages, all pairs)."""
+    _check(load_library().tl_kv_copy(_cache_ref(cache), _ptr(src), _ptr(dst), _ptr(tokens), _ptr(count), max_pairs,
+                                     _stream(stream)), "tl_kv_copy")
+
+
 def tl_attn(Q, ldq, cache, page_table, max_pages, lens, q_offsets, mask, mask_words, num_seqs, total_q, max_q, max_len,
             q_heads, scale, O, stream=None):
     """mask may be None (causal)."""
@@ -647,6 +710,90 @@ def kv_keep(cache: KVCache, page_table, starts, path, counts, stream=None):
     if starts.numel() != B or counts.numel() != B or path.shape[0] != B:
         raise ValueError("one row per sequence")
     tl_kv_keep(cache, page_table, page_table.shape[1], starts, path, path.shape[1], counts, B, stream)
+
+
+def kv_pages(num_pages, rows, max_pages, page_tokens=64, device="cuda") -> KVPages:
+    """A pool of free pages, and a table of rows that hold none."""
+    import torch
+    return KVPages(torch.zeros(num_pages, dtype=torch.int32, device=device),
+                   torch.full((rows, max_pages), -1, dtype=torch.int32, device=device), page_tokens)
+
+
+def _lists(n, device, given, *sizes):
+    """int32 outputs of the given sizes: those given, checked, or new ones."""
+    import torch
+    if given is None:
+        return tuple(torch.empty(x, dtype=torch.int32, device=device) for x in sizes)
+    _int32(*given)
+    if [x.numel() for x in given] != list(sizes):
+        raise ValueError(f"out holds {sizes} values")
+    return given
+
+
+def kv_grow(pages: KVPages, rows, lens, missing=None, stream=None):
+    """Pages for the first lens[i] tokens of row rows[i] of the table (int32 [n] both), where it has none; returns int32 [1]:
+    how many entries found no free page."""
+    rc = (_calls or _load_calls()).kv_grow(pages.desc, rows, lens, missing, stream)
+    if rc is not None:
+        return missing if rc == TL_OK else _check(rc, "tl_kv_grow")
+    _int32(rows, lens)
+    if rows.numel() != lens.numel():
+        raise ValueError("one length per row")
+    missing, = _lists(rows.numel(), pages.refs.device, None if missing is None else (missing,), 1)
+    tl_kv_grow(pages, rows, lens, rows.numel(), missing, stream)
+    return missing
+
+
+def kv_free(pages: KVPages, rows, lens=None, stream=None):
+    """Rows of the table (int32 [n]) give their pages back, but for those of their first lens[i] tokens."""
+    rc = (_calls or _load_calls()).kv_free(pages.desc, rows, lens, stream)
+    if rc is not None:
+        return _check(rc, "tl_kv_free")
+    _int32(rows, lens)
+    if lens is not None and rows.numel() != lens.numel():
+        raise ValueError("one length per row")
+    tl_kv_free(pages, rows, lens, rows.numel(), stream)
+
+
+def kv_fork(pages: KVPages, parents, children, lens, out=None, stream=None):
+    """Row children[i] of the table goes on from the first lens[i] tokens of row parents[i].  Returns (src, dst, tokens, count),
+    the pairs of pages that kv_copy copies in every cache of the pool: int32 [n] three times, and [2]: the pairs, and the
+    children for which no page was free."""
+    src, dst, tokens, count = out if out is not None else (None,) * 4
+    rc = (_calls or _load_calls()).kv_fork(pages.desc, parents, children, lens, src, dst, tokens, count, stream)
+    if rc is not None:
+        return out if rc == TL_OK else _check(rc, "tl_kv_fork")
+    _int32(parents, children, lens)
+    n = children.numel()
+    if parents.numel() != n or lens.numel() != n:
+        raise ValueError("one parent and one length per child")
+    out = _lists(n, pages.refs.device, out, n, n, n, 2)
+    tl_kv_fork(pages, parents, children, lens, n, *out, stream)
+    return out
+
+
+def kv_compact(pages: KVPages, max_moves, out=None, stream=None):
+    """Moves pages in use to the front of the pool, max_moves of them at most.  Returns (src, dst, count), which kv_copy takes
+    for every cache of the pool: int32 [max_moves] twice, and [2]: the moves, and the pages in use."""
+    src, dst, count = out if out is not None else (None,) * 3
+    rc = (_calls or _load_calls()).kv_compact(pages.desc, max_moves, src, dst, count, stream)
+    if rc is not None:
+        return out if rc == TL_OK else _check(rc, "tl_kv_compact")
+    out = _lists(max_moves, pages.refs.device, out, max_moves, max_moves, 2)
+    tl_kv_compact(pages, max_moves, *out, stream)
+    return out
+
+
+def kv_copy(cache: KVCache, src, dst, tokens=None, count=None, stream=None):
+    """Copies pages src[i] to dst[i] (int32 [n]): their first tokens[i] tokens (None: all), the first count[0] pairs (None: all)."""
+    rc = (_calls or _load_calls()).kv_copy(cache.desc, src, dst, tokens, count, stream)
+    if rc is not None:
+        return _check(rc, "tl_kv_copy")
+    _int32(src, dst, tokens, count)
+    n = src.numel()
+    if dst.numel() != n or (tokens is not None and tokens.numel() != n) or (count is not None and count.numel() < 1):
+        raise ValueError("one destination, and one number of tokens, per source")
+    tl_kv_copy(cache, src, dst, tokens, count, n, stream)
 
 
 def attention(q, cache: KVCache, page_table, lens, q_offsets, max_q, max_len, scale, mask=None, out=None, stream=None):

@@ -1,0 +1,450 @@
+// The pages of a key/value cache: handing them out, forking, giving back,
+// compacting, and copying what they hold.
+//
+// Free pages go out in rising order, so that every call has one right answer:
+// the pages that nobody refers to become a map of bits, 4096 pages a wave, with
+// their number (page_map); the r-th free one is then found by a scan of the
+// numbers and one of a block's bits.  What a call hands out it takes from that
+// map, so that references may change meanwhile.  Tables and references change by
+// exchanges and sums, in whose order nothing depends: every entry of a table
+// holds one reference to its page before and after, also where rows are named
+// twice.
+//
+// A call is a chain of phases, each of which needs the one before whole: as
+// launches, or, where there is little to do, one after the other in one
+// workgroup (a launch costs 2.6 us, a barrier nothing).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "tl_serve.h"
+#include "tl_serve_device.h"
+
+namespace tl {
+namespace {
+
+constexpr int kThreads = kPageThreads;
+constexpr int kWide = 1024;             // threads of a call that is one workgroup
+constexpr int kBlock = kPageBlock;      // pages of a wave's bits: a word of 64 a lane
+typedef unsigned long long u64;
+
+// the waves of a phase, and the sums that they take over their lanes
+struct Crew {
+    int64_t wave, waves;
+    int lane;
+};
+__device__ inline Crew crew() {
+    return Crew{int64_t(blockIdx.x) * (blockDim.x / 64) + threadIdx.x / 64, int64_t(gridDim.x) * (blockDim.x / 64), int(threadIdx.x & 63)};
+}
+__device__ inline int before_lane(int x, int lane) {       // sum over the lanes before
+    int sum = x;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int y = __shfl_up(sum, d);
+        if (lane >= d) sum += y;
+    }
+    return sum - x;
+}
+__device__ inline int over_lanes(int x) {
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
+    return x;
+}
+
+// LDS that a wave's lanes write for one another
+__device__ inline void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// Bits of the free pages and their number, block after block.
+__device__ inline void page_map(const PagesLaunch& a, const Crew& w, int64_t first_wave) {
+    for (int64_t b = w.wave - first_wave; b < a.blocks; b += w.waves) {
+        if (b < 0) continue;
+        const int64_t base = b * kBlock;
+        u64 mine = 0;
+#pragma unroll
+        for (int part = 0; part < 4; ++part) {
+            int refs[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const int64_t page = base + (part * 16 + j) * 64 + w.lane;
+                refs[j] = a.refs[min(page, a.num_pages - 1)];
+            }
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const u64 bits = __ballot(refs[j] == 0 && base + (part * 16 + j) * 64 + w.lane < a.num_pages);
+                if (w.lane == part * 16 + j) mine = bits;
+            }
+        }
+        a.map[b * 64 + w.lane] = mine;
+        const int free = over_lanes(__popcll(mine));
+        if (w.lane == 0) a.free[b] = free;
+    }
+}
+
+// Where the r-th free page is, for ever larger r: the block, and the free pages
+// before it.
+struct PageCursor {
+    int64_t block;
+    int64_t before;
+};
+__device__ inline int free_in(const PagesLaunch& a, int64_t b) { return b < a.blocks ? a.free[b] : 0; }
+// the first block with the r-th free page in it or before its end; blocks: there is none
+__device__ inline void page_seek(const PagesLaunch& a, const Crew& w, int64_t r, PageCursor* c) {
+    while (c->block < a.blocks) {
+        const int n = free_in(a, c->block + w.lane), upto = before_lane(n, w.lane) + n;
+        const u64 past = __ballot(c->before + upto > r);
+        if (past) {
+            const int at = __builtin_ctzll(past);
+            c->before += __shfl(upto - n, at);
+            c->block += at;
+            return;
+        }
+        c->before += __shfl(upto, 63);
+        c->block += 64;
+    }
+    c->block = a.blocks;
+}
+// Free pages of rank [r, r + count), count <= 64, to 'to' in LDS; returns how many there are.
+__device__ inline int page_take(const PagesLaunch& a, const Crew& w, int64_t r, int count, PageCursor* c, int32_t* to) {
+    int got = 0;
+    while (got < count) {
+        page_seek(a, w, r + got, c);
+        if (c->block >= a.blocks) break;
+        u64 bits = a.map[c->block * 64 + w.lane];
+        const int n = __popcll(bits), at = before_lane(n, w.lane);
+        int64_t rank = c->before + at;
+        const int64_t end = r + count;
+        if (rank < end && rank + n > r) {
+            for (; bits; bits &= bits - 1, ++rank)
+                if (rank >= r && rank < end) to[rank - r] = int32_t(c->block * kBlock + w.lane * 64 + __builtin_ctzll(bits));
+        }
+        const int64_t block_end = c->before + over_lanes(n);
+        got = int(min(end, block_end) - r);
+    }
+    wave_sync();
+    return got;
+}
+__device__ inline int64_t all_free(const PagesLaunch& a, const Crew& w) {
+    int sum = 0;
+    for (int64_t b = w.lane; b < a.blocks; b += 64) sum += a.free[b];
+    return over_lanes(sum);
+}
+// the wants of the sequences before i
+__device__ inline int64_t wants_before(const PagesLaunch& a, const Crew& w, int64_t i) {
+    int64_t sum = 0;
+    for (int64_t j = w.lane; j < i; j += 64) sum += a.want[j];
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor((long long)sum, d);
+    return sum;
+}
+
+__device__ inline int pages_of(const PagesLaunch& a, int len) { return int(min(a.max_pages, (int64_t(max(len, 0)) + (1 << a.log2_page) - 1) >> a.log2_page)); }
+__device__ inline int32_t* row_of(const PagesLaunch& a, int row) { return row >= 0 && row < a.num_rows ? a.table + row * a.max_pages : nullptr; }
+__device__ inline bool is_page(const PagesLaunch& a, int page) { return page >= 0 && page < a.num_pages; }
+// a table's entry lets go of a page
+__device__ inline void let_go(const PagesLaunch& a, int page) {
+    if (is_page(a, page)) atomicSub(&a.refs[page], 1);
+}
+
+// grow, first phase: how many entries of each row need a page, and the first of them
+__device__ void grow_count(const PagesLaunch& a, const Crew& w) {
+    for (int64_t i = w.wave; i < a.n; i += w.waves) {
+        const int32_t* row = row_of(a, a.rows[i]);
+        const int need = row ? pages_of(a, a.lens[i]) : 0;
+        int count = 0, first = need;
+        for (int base = 0; base < need; base += 64 * 8) {
+            int page[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) page[j] = row[min(base + 64 * j + w.lane, need - 1)];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const u64 none = __ballot(page[j] < 0 && base + 64 * j + w.lane < need);
+                if (none && first == need) first = base + 64 * j + __builtin_ctzll(none);
+                count += __popcll(none);
+            }
+        }
+        if (w.lane == 0) a.want[i] = count, a.first[i] = first;
+    }
+}
+// second phase: the pages
+__device__ void grow_give(const PagesLaunch& a, const Crew& w, int32_t* pages) {
+    for (int64_t i = w.wave; i < max(a.n, int64_t(1)); i += w.waves) {
+        const int want = a.n ? a.want[i] : 0;
+        if (want == 0 && i < a.n - 1) continue;
+        int64_t rank = wants_before(a, w, i);
+        if (i >= a.n - 1) {                                 // the last one knows them all
+            const int64_t missing = rank + want - all_free(a, w);
+            if (w.lane == 0) *a.count = int32_t(max(int64_t(0), missing));
+        }
+        if (want == 0) continue;
+        int32_t* row = row_of(a, a.rows[i]);
+        const int need = pages_of(a, a.lens[i]);
+        PageCursor c{0, 0};
+        for (int base = a.first[i]; base < need; base += 64) {
+            const int old = base + w.lane < need ? row[base + w.lane] : 0;
+            const u64 none = __ballot(old < 0);
+            if (!none) continue;
+            const int got = page_take(a, w, rank, __popcll(none), &c, pages);
+            const int mine = __popcll(none & ((1ull << w.lane) - 1));
+            // a row that is named twice: the one that comes second leaves its page free
+            if (old < 0 && mine < got && atomicCAS(&row[base + w.lane], old, pages[mine]) == old) a.refs[pages[mine]] = 1;
+            rank += __popcll(none);
+            wave_sync();
+            if (got < __popcll(none)) break;
+        }
+    }
+}
+
+// fork, first phase: which children need a page of their own
+__device__ void fork_count(const PagesLaunch& a, const Crew& w) {
+    for (int64_t i = w.wave * 64 + w.lane; i < a.n; i += w.waves * 64) {
+        const int32_t* from = row_of(a, a.parents[i]);
+        const int64_t len = min(int64_t(max(a.lens[i], 0)), a.max_pages << a.log2_page), full = len >> a.log2_page;
+        const bool part = from && row_of(a, a.rows[i]) && (len & ((1 << a.log2_page) - 1));
+        a.want[i] = part && is_page(a, from[full]) ? 1 : 0;
+    }
+}
+// second phase: the children's rows, and the pairs to copy
+__device__ void fork_give(const PagesLaunch& a, const Crew& w, int32_t* pages) {
+    for (int64_t i = w.wave; i < max(a.n, int64_t(1)); i += w.waves) {
+        const int want = a.n ? a.want[i] : 0;
+        const bool last = i >= a.n - 1;
+        const int64_t rank = want || last ? wants_before(a, w, i) : 0;
+        if (last) {
+            const int64_t all = rank + want, free = all_free(a, w), pairs = min(all, free);
+            if (w.lane == 0) a.count[0] = int32_t(pairs), a.count[1] = int32_t(all - pairs);
+            for (int64_t j = pairs + w.lane; j < a.n; j += 64) a.src[j] = a.dst[j] = a.tokens[j] = -1;
+            if (a.n == 0) continue;
+        }
+        const int32_t* from = row_of(a, a.parents[i]);
+        int32_t* to = row_of(a, a.rows[i]);
+        if (!to) continue;
+        const int64_t len = from ? min(int64_t(max(a.lens[i], 0)), a.max_pages << a.log2_page) : 0;
+        const int full = int(len >> a.log2_page);
+        int own = -1;
+        if (want) {
+            PageCursor c{0, 0};
+            if (page_take(a, w, rank, 1, &c, pages)) own = pages[0];
+            wave_sync();
+            if (own >= 0 && w.lane == 0) {
+                a.src[rank] = from[full];
+                a.dst[rank] = own;
+                a.tokens[rank] = int32_t(len & ((1 << a.log2_page) - 1));
+                atomicAdd(&a.refs[own], 1);
+            }
+        }
+        for (int64_t base = 0; base < a.max_pages; base += 64 * 4) {
+            int page[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int64_t at = base + 64 * j + w.lane;
+                page[j] = at < full ? from[at] : at == full ? own : -1;
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int64_t at = base + 64 * j + w.lane;
+                if (at >= a.max_pages) continue;
+                const int page_here = is_page(a, page[j]) ? page[j] : -1;
+                if (at < full && page_here >= 0) atomicAdd(&a.refs[page_here], 1);
+                let_go(a, atomicExch(&to[at], page_here));
+            }
+        }
+    }
+}
+
+// compact, second phase: of U pages in use, the M that lie behind the first U
+// pages, from the last one on, go to the free ones among those, from the first
+// one on.  With f(p) free pages before p, page p is the (U - 1 - (p - f(p)))-th
+// in use from the end.
+struct CompactSizes {
+    int64_t used, moves;
+};
+__device__ inline CompactSizes compact_sizes(const PagesLaunch& a, const Crew& w) {
+    CompactSizes s;
+    s.used = a.num_pages - all_free(a, w);
+    const int64_t block = s.used / kBlock;      // of page U
+    int64_t before = 0;
+    for (int64_t b = w.lane; b < min(block, a.blocks); b += 64) before += a.free[b];
+    if (block < a.blocks) {
+        const int64_t left = s.used - block * kBlock - w.lane * 64;     // pages of this lane's word before page U
+        const u64 bits = a.map[block * 64 + w.lane] & (left <= 0 ? 0 : left >= 64 ? ~0ull : (1ull << left) - 1);
+        before += __popcll(bits);
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) before += __shfl_xor((long long)before, d);
+    s.moves = min(before, a.n);
+    return s;
+}
+__device__ void compact_list(const PagesLaunch& a, const Crew& w) {
+    if (w.wave >= a.blocks && w.wave > 0) return;
+    const CompactSizes s = compact_sizes(a, w);
+    if (w.wave == 0 && w.lane == 0) a.count[0] = int32_t(s.moves), a.count[1] = int32_t(s.used);
+    const int64_t crew = min(w.waves, a.blocks);
+    for (int64_t k = s.moves + w.wave * 64 + w.lane; k < a.n; k += crew * 64) a.src[k] = a.dst[k] = -1;
+    int64_t before_block = 0, at = 0;
+    for (int64_t b = w.wave; b < a.blocks; b += w.waves) {
+        int64_t sum = 0;
+        for (int64_t j = at + w.lane; j < b; j += 64) sum += a.free[j];
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) sum += __shfl_xor((long long)sum, d);
+        before_block += sum;
+        at = b;
+        const u64 mine = a.map[b * 64 + w.lane];
+        const int before = before_lane(__popcll(mine), w.lane);
+        // word after word, a page a lane
+        for (int j = 0; j < 64 && b * kBlock + j * 64 < a.num_pages; ++j) {
+            const u64 bits = __shfl((long long)mine, j);
+            const int64_t page = b * kBlock + j * 64 + w.lane, f = before_block + __shfl(before, j) + __popcll(bits & ((1ull << w.lane) - 1));
+            if (page >= a.num_pages) continue;
+            const bool free = bits >> w.lane & 1;
+            if (free && page < s.used && f < s.moves) a.dst[f] = int32_t(page);
+            const int64_t k = s.used - 1 - (page - f);
+            if (!free && page >= s.used) {
+                a.name[page] = int32_t(k < s.moves ? k : -1);
+                if (k < s.moves) a.src[k] = int32_t(page);
+            }
+        }
+    }
+}
+// third phase: references and tables follow
+__device__ void compact_apply(const PagesLaunch& a, const Crew& w) {
+    const int64_t moves = a.count[0], used = a.count[1], thread = w.wave * 64 + w.lane, threads = w.waves * 64;
+    for (int64_t k = thread; k < moves; k += threads) {
+        a.refs[a.dst[k]] = a.refs[a.src[k]];
+        a.refs[a.src[k]] = 0;
+    }
+    const int64_t entries = int64_t(a.num_rows) * a.max_pages;
+    for (int64_t i = thread; i < entries; i += threads) {
+        const int page = a.table[i];
+        if (page < used || page >= a.num_pages || a.map[page / 64] >> (page % 64) & 1) continue;
+        const int k = a.name[page];
+        if (k >= 0) a.table[i] = a.dst[k];
+    }
+}
+
+// what the phases before wrote is there for those after, in one workgroup
+__device__ inline void next_phase() {
+    __threadfence_block();
+    __syncthreads();
+}
+
+template <int OP, int PHASE>       // PHASE 0: all of them
+__global__ __launch_bounds__(PHASE ? kThreads : kWide) void pages_kernel(PagesLaunch a) {
+    __shared__ int32_t pages_s[(PHASE ? kThreads : kWide) / 64][64];
+    const Crew w = crew();
+    int32_t* pages = pages_s[threadIdx.x / 64];
+    if (PHASE <= 1) {
+        if (OP == kPagesGrow) grow_count(a, w);
+        if (OP == kPagesFork) fork_count(a, w);
+        page_map(a, w, PHASE == 1 ? a.map_wave : 0);
+    }
+    if (PHASE == 0) next_phase();
+    if (PHASE == 0 || PHASE == 2) {
+        if (OP == kPagesGrow) grow_give(a, w, pages);
+        if (OP == kPagesFork) fork_give(a, w, pages);
+        if (OP == kPagesCompact) compact_list(a, w);
+    }
+    if (PHASE == 0) next_phase();
+    if ((PHASE == 0 || PHASE == 3) && OP == kPagesCompact) compact_apply(a, w);
+}
+
+// free: a row's entries from the len-th token's page on, 64 at a time
+__global__ __launch_bounds__(kThreads) void pages_free_kernel(PagesLaunch a, int parts) {
+    const Crew w = crew();
+    const int64_t i = w.wave / parts;
+    if (i >= a.n) return;
+    int32_t* row = row_of(a, a.rows[i]);
+    if (!row) return;
+    const int64_t at = (a.lens ? pages_of(a, a.lens[i]) : 0) + (w.wave - i * parts) * 64 + w.lane;
+    for (int64_t j = at; j < a.max_pages; j += int64_t(parts) * 64)
+        if (row[j] != -1) let_go(a, atomicExch(&row[j], -1));
+}
+
+// ---------------------------------------------------------------------------
+// copy: a workgroup takes 64 tokens of a head of a pair of pages, one run of
+// bytes in each of the cache's arrays.
+// ---------------------------------------------------------------------------
+template <int BYTES, int EXPS>      // of a token's head: of keys (and of values), and their exponents
+__global__ __launch_bounds__(kThreads) void pages_copy_kernel(PagesCopyLaunch a) {
+    constexpr int kChunks = 64 * BYTES / 16, kLoads = (kChunks + kThreads - 1) / kThreads;
+    const int log2_groups = a.c.log2_page - 6, per = a.c.heads << log2_groups;
+    const int64_t pairs = a.count ? min(max(int64_t(*a.count), int64_t(0)), a.pairs) : a.pairs;
+    for (int64_t u = blockIdx.x; u < pairs * per; u += gridDim.x) {
+        const int64_t pair = u / per;
+        const int rest = int(u - pair * per), group = rest & ((1 << log2_groups) - 1);
+        const int64_t src = a.src[pair], dst = a.dst[pair];
+        if (src < 0 || src >= a.c.num_pages || dst < 0 || dst >= a.c.num_pages || src == dst) continue;
+        if (a.tokens && group * 64 >= a.tokens[pair]) continue;
+        const int64_t from = (src * per + rest) * 64, to = (dst * per + rest) * 64;        // tokens of one head
+        const u32x4 *k0 = reinterpret_cast<const u32x4*>(a.c.k + from * BYTES), *v0 = reinterpret_cast<const u32x4*>(a.c.v + from * BYTES);
+        u32x4 *k1 = reinterpret_cast<u32x4*>(a.c.k + to * BYTES), *v1 = reinterpret_cast<u32x4*>(a.c.v + to * BYTES);
+        u32x4 k[kLoads], v[kLoads], e = {0, 0, 0, 0};
+        // exponents: 4 EXPS chunks of the keys', then of the values'
+        const int chunk = threadIdx.x % (EXPS ? 4 * EXPS : 1), which = threadIdx.x / (EXPS ? 4 * EXPS : 1);
+        uint8_t* exps = which ? a.c.v_exp : a.c.k_exp;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int x = i * kThreads + threadIdx.x;
+            if (kChunks % kThreads && x >= kChunks) break;
+            k[i] = k0[x], v[i] = v0[x];
+        }
+        if (EXPS && which < 2) e = reinterpret_cast<const u32x4*>(exps + from * EXPS)[chunk];
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int x = i * kThreads + threadIdx.x;
+            if (kChunks % kThreads && x >= kChunks) break;
+            k1[x] = k[i], v1[x] = v[i];
+        }
+        if (EXPS && which < 2) reinterpret_cast<u32x4*>(exps + to * EXPS)[chunk] = e;
+    }
+}
+
+uint32_t groups_of(int64_t waves) { return uint32_t(std::max<int64_t>(1, (waves + kThreads / 64 - 1) / (kThreads / 64))); }
+
+template <int OP>
+hipError_t launch_phases(const PagesLaunch& given, int64_t first, int64_t second, int64_t third, hipStream_t stream) {
+    PagesLaunch a = given;
+    // one workgroup of sixteen waves where none has more than a few things to do
+    if (first + a.blocks <= 64 && second <= 64 && third <= 512) {
+        hipLaunchKernelGGL((pages_kernel<OP, 0>), dim3(1), dim3(kWide), 0, stream, a);
+        return hipGetLastError();
+    }
+    a.map_wave = first;
+    hipLaunchKernelGGL((pages_kernel<OP, 1>), dim3(groups_of(first + a.blocks)), dim3(kThreads), 0, stream, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((pages_kernel<OP, 2>), dim3(groups_of(second)), dim3(kThreads), 0, stream, a);
+    e = hipGetLastError();
+    if (e != hipSuccess || !third) return e;
+    hipLaunchKernelGGL((pages_kernel<OP, 3>), dim3(groups_of(std::min<int64_t>(third, 4096))), dim3(kThreads), 0, stream, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_pages_grow(const PagesLaunch& a, hipStream_t stream) { return launch_phases<kPagesGrow>(a, a.n, a.n, 0, stream); }
+hipError_t launch_pages_fork(const PagesLaunch& a, hipStream_t stream) { return launch_phases<kPagesFork>(a, (a.n + 63) / 64, a.n, 0, stream); }
+hipError_t launch_pages_compact(const PagesLaunch& a, hipStream_t stream) {
+    return launch_phases<kPagesCompact>(a, 0, a.blocks, std::max((int64_t(a.num_rows) * a.max_pages + 63) / 64, (a.n + 63) / 64), stream);
+}
+
+hipError_t launch_pages_free(const PagesLaunch& a, hipStream_t stream) {
+    // entries of a row for a wave: 256, and more than that only where the launch would be too large
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>((a.max_pages + 255) / 256, (int64_t(1) << 22) / a.n));
+    hipLaunchKernelGGL(pages_free_kernel, dim3(groups_of(a.n * parts)), dim3(kThreads), 0, stream, a, int(parts));
+    return hipGetLastError();
+}
+
+hipError_t launch_pages_copy(const PagesCopyLaunch& a, int head_dim, int elem_bytes, hipStream_t stream) {
+    const int64_t units = a.pairs * a.c.heads << (a.c.log2_page - 6);
+    return kv_as(head_dim, elem_bytes, [&](auto d, auto e) {
+        constexpr int D = d(), E = e();
+        hipLaunchKernelGGL((pages_copy_kernel<kv_width<D, E>() * kv_size<E>(), kv_exps<D, E>()>), dim3(uint32_t(std::min<int64_t>(units, 2048))),
+                           dim3(kThreads), 0, stream, a);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace tl

@@ -1,6 +1,6 @@
 // Internal declarations of the serving-step operators: the paged key/value
-// cache (tl_kv.hip), attention over it (tl_attn.hip) and the verification of
-// drafted tokens (tl_verify.hip).  The entry points in tl_serve.cpp check all
+// cache (tl_kv.hip), its pages (tl_pages.hip), attention over it (tl_attn.hip)
+// and the verification of drafted tokens (tl_verify.hip).  The entry points in tl_serve.cpp check all
 // arguments; the launchers only enqueue.
 #pragma once
 
@@ -117,6 +117,51 @@ struct KvKeepLaunch {
     int num_seqs, max_path;
 };
 hipError_t launch_kv_keep(const KvKeepLaunch& a, int head_dim, int elem_bytes, hipStream_t stream);
+
+// A call on a pool of pages (tl_pages.hip).
+constexpr int kPagesGrow = 0, kPagesFork = 1, kPagesCompact = 2;
+constexpr int kPageThreads = 256;
+constexpr int kPageBlock = 4096;    // pages whose bits a wave makes
+constexpr int kMostPageRows = 65536;
+struct PagesLaunch {
+    int32_t* refs;
+    int32_t* table;             // [num_rows][max_pages]
+    int64_t num_pages, max_pages;
+    int num_rows;
+    int log2_page;
+    int64_t n;                  // sequences (compact: moves at most)
+    const int32_t* rows;        // the sequences' rows; fork: the children's
+    const int32_t* parents;
+    const int32_t* lens;
+    int32_t* src;
+    int32_t* dst;
+    int32_t* tokens;
+    int32_t* count;             // grow: missing
+    // workspace: bits of the free pages and their number per block of pages; of
+    // each sequence the pages that it wants, and the first entry without one;
+    // of each page its place in the list of moves
+    int64_t blocks;
+    unsigned long long* map;
+    int32_t* free;
+    int32_t* want;
+    int32_t* first;
+    int32_t* name;
+    int64_t map_wave;           // the first wave of a launch that makes bits
+};
+hipError_t launch_pages_grow(const PagesLaunch& a, hipStream_t stream);
+hipError_t launch_pages_free(const PagesLaunch& a, hipStream_t stream);
+hipError_t launch_pages_fork(const PagesLaunch& a, hipStream_t stream);
+hipError_t launch_pages_compact(const PagesLaunch& a, hipStream_t stream);
+
+struct PagesCopyLaunch {
+    KvView c;
+    const int32_t* src;
+    const int32_t* dst;
+    const int32_t* tokens;      // nullptr: whole pages
+    const int32_t* count;       // nullptr: all pairs
+    int64_t pairs;
+};
+hipError_t launch_pages_copy(const PagesCopyLaunch& a, int head_dim, int elem_bytes, hipStream_t stream);
 
 struct AttnLaunch {
     KvView c;

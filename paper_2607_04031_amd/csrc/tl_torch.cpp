@@ -187,6 +187,87 @@ int kv_keep(PyObject* const* a) {
     return rc;
 }
 
+// int32 lists of n entries each, none of them missing
+int32_t* list(PyObject* x, int device, int64_t n) { return ints(tensor(x, device), n); }
+
+// pages descriptor, rows, lens, missing, stream
+int kv_grow(PyObject* const* a) {
+    const Where here(a[4]);
+    const auto pages = structure<tl_kv_pages>(a[0]);
+    const int64_t n = tensor(a[1], here.device).numel();
+    need(n <= INT32_MAX);
+    const int32_t *rows = list(a[1], here.device, n), *lens = list(a[2], here.device, n);
+    int32_t* missing = list(a[3], here.device, 1);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = tl_kv_grow(&pages, rows, lens, int32_t(n), missing, here.stream);
+    Py_END_ALLOW_THREADS
+    return rc;
+}
+
+// pages descriptor, rows, lens, stream
+int kv_free(PyObject* const* a) {
+    const Where here(a[3]);
+    const auto pages = structure<tl_kv_pages>(a[0]);
+    const int64_t n = tensor(a[1], here.device).numel();
+    need(n <= INT32_MAX);
+    const int32_t *rows = list(a[1], here.device, n), *lens = a[2] == Py_None ? nullptr : list(a[2], here.device, n);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = tl_kv_free(&pages, rows, lens, int32_t(n), here.stream);
+    Py_END_ALLOW_THREADS
+    return rc;
+}
+
+// pages descriptor, parents, children, lens, src, dst, tokens, count, stream
+int kv_fork(PyObject* const* a) {
+    const Where here(a[8]);
+    const auto pages = structure<tl_kv_pages>(a[0]);
+    const int64_t n = tensor(a[2], here.device).numel();
+    need(n <= INT32_MAX);
+    int32_t* lists[6];
+    for (int i = 0; i < 6; ++i) lists[i] = list(a[1 + i], here.device, n);
+    int32_t* count = list(a[7], here.device, 2);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = tl_kv_fork(&pages, lists[0], lists[1], lists[2], int32_t(n), lists[3], lists[4], lists[5], count, here.stream);
+    Py_END_ALLOW_THREADS
+    return rc;
+}
+
+// pages descriptor, max_moves, src, dst, count, stream
+int kv_compact(PyObject* const* a) {
+    const Where here(a[5]);
+    const auto pages = structure<tl_kv_pages>(a[0]);
+    const int64_t n = number(a[1]);
+    int32_t *src = list(a[2], here.device, n), *dst = list(a[3], here.device, n), *count = list(a[4], here.device, 2);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = tl_kv_compact(&pages, n, src, dst, count, here.stream);
+    Py_END_ALLOW_THREADS
+    return rc;
+}
+
+// cache descriptor, src, dst, tokens, count, stream
+int kv_copy(PyObject* const* a) {
+    const Where here(a[5]);
+    const auto cache = structure<tl_kv_cache>(a[0]);
+    const int64_t n = tensor(a[1], here.device).numel();
+    const int32_t *src = list(a[1], here.device, n), *dst = list(a[2], here.device, n);
+    const int32_t* tokens = a[3] == Py_None ? nullptr : list(a[3], here.device, n);
+    const int32_t* count = nullptr;
+    if (a[4] != Py_None) {
+        const int64_t size = tensor(a[4], here.device).numel();
+        need(size >= 1);
+        count = list(a[4], here.device, size);
+    }
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = tl_kv_copy(&cache, src, dst, tokens, count, n, here.stream);
+    Py_END_ALLOW_THREADS
+    return rc;
+}
+
 // q, cache descriptor, page_table, lens, q_offsets, max_q, max_len, scale, mask, out, stream
 int attention(PyObject* const* a) {
     const Where here(a[10]);
@@ -263,7 +344,8 @@ PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t count) {
 
 #define FUNCTION(name, count) \
     { #name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&call<name, count>)), METH_FASTCALL, nullptr }
-PyMethodDef functions[] = {FUNCTION(kv_append, 8), FUNCTION(kv_read, 5), FUNCTION(kv_keep, 6), FUNCTION(attention, 11), FUNCTION(verify, 13), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef functions[] = {FUNCTION(kv_append, 8), FUNCTION(kv_read, 5), FUNCTION(kv_keep, 6), FUNCTION(kv_grow, 5), FUNCTION(kv_free, 4),
+                           FUNCTION(kv_fork, 9), FUNCTION(kv_compact, 6), FUNCTION(kv_copy, 6), FUNCTION(attention, 11), FUNCTION(verify, 13), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tl_torch", nullptr, -1, functions, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
