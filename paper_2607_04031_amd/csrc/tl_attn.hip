@@ -151,6 +151,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
         auto step = [&](auto is_masked) {
             constexpr bool masked = decltype(is_masked)::value;
             const int left = block < 0 ? 0 : s.len - chunk * kKeys - 4 * g;        // this lane's key 16 mb + i exists below that
+            bool odd_exps = false;      // 4 bits: some value of the wave's may be infinite or NaN
 #pragma unroll
             for (int part = 0; part < kParts; ++part) {
                 // S^T: keys 16 mb + 4 g + i of the chunk, row col
@@ -199,6 +200,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
                         for (int i = 0; i < kLoads; ++i)
 #pragma unroll
                             for (int mb = 0; mb < kBlocks; ++mb) v_exp4[kFour ? i : 0][mb] &= attn_first_bytes(left - 16 * mb);
+                        uint32_t some = 0;
+#pragma unroll
+                        for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+                            for (int mb = 0; mb < kBlocks; ++mb) some |= attn_odd_exps(v_exp4[kFour ? i : 0][mb]);
+                        odd_exps = __ballot(some) != 0;
                     }
                     if (part == 0 && !kFour) {
 #pragma unroll
@@ -262,7 +269,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
                             const u32x4 e = v_exp4[kFour ? i : 0];
                             u32x4 vf[2];
                             attn_values4(vw[i][m & 3], vw[i][(m + 1) & 3], e[m & 3], e[(m + 1) & 3], &vf[0], &vf[1]);
-                            if (masked) {
+                            if (masked && odd_exps) {
 #pragma unroll
                                 for (int j = 0; j < 8; ++j) {
                                     const uint32_t bad = attn_odd<2>(vf[j / 4][j % 4]);

@@ -374,6 +374,10 @@ __device__ inline int attn_key4_exp(int lane) { return (lane >> 4) * D / 128 * 6
 // conversions do not look at, are what comes along.
 __device__ inline float attn_exp4(uint32_t exps, int i) { return __uint_as_float(i < 3 ? exps << (23 - 8 * i) : exps >> 1); }
 
+// Whether some of four scales make infinities (2^126 and 2^127) or NaNs of codes:
+// nonzero.  Without them, values need not be looked at one by one.
+__device__ inline uint32_t attn_odd_exps(uint32_t e) { return ((e & 0x7f7f7f7fu) + 0x03030303u) & e & 0x80808080u; }
+
 // Values of 32 keys: dwords of the keys 16 m + 4 g + i (m = 0, 1) hold elements d
 // and d + 16 of key i in byte i, exps their scales.  Operands of O^T = V^T P^T for
 // the 16 elements of the head from d on, and from d + 16 on.

@@ -172,15 +172,20 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
                 const float scale = attn_exp4(k_exp >> (8 * wave), 0);
 #pragma unroll
                 for (int f = 0; f < kSteps; ++f) ks[(wave * kSteps + f) * 64] = fp4_to_bf16x8(kw4.step[f], scale);
+                uint32_t some = 0;
                 if (masked) {           // any code is a finite number, under a finite scale
 #pragma unroll
-                    for (int m = 0; m < 2 * kHalves; ++m) v_exp4[m] &= attn_first_bytes(s.len - chunk * kKeys - 4 * g - 16 * (2 * value_half + m));
+                    for (int m = 0; m < 2 * kHalves; ++m) {
+                        v_exp4[m] &= attn_first_bytes(s.len - chunk * kKeys - 4 * g - 16 * (2 * value_half + m));
+                        some |= attn_odd_exps(v_exp4[m]);
+                    }
                 }
+                const bool odd_exps = masked && __ballot(some);
 #pragma unroll
                 for (int h = 0; h < kHalves; ++h) {
                     u32x4 vf[2];
                     attn_values4(vw4[2 * h], vw4[2 * h + 1], v_exp4[2 * h], v_exp4[2 * h + 1], &vf[0], &vf[1]);
-                    if (masked) {
+                    if (odd_exps) {
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
                             const uint32_t bad = attn_odd<2>(vf[j / 4][j % 4]);
