@@ -24,7 +24,8 @@ namespace tl {
 namespace {
 
 constexpr int kThreads = kPageThreads;
-constexpr int kWide = 1024;             // threads of a call that is one workgroup
+constexpr int kWide = 1024;             // threads of a call that is one workgroup, for so many blocks and sequences
+constexpr int kFewBlocks = 16, kFewRows = 64;
 constexpr int kBlock = kPageBlock;      // pages of a wave's bits: a word of 64 a lane
 typedef unsigned long long u64;
 
@@ -36,19 +37,42 @@ struct Crew {
 __device__ inline Crew crew() {
     return Crew{int64_t(blockIdx.x) * (blockDim.x / 64) + threadIdx.x / 64, int64_t(gridDim.x) * (blockDim.x / 64), int(threadIdx.x & 63)};
 }
-__device__ inline int before_lane(int x, int lane) {       // sum over the lanes before
-    int sum = x;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int y = __shfl_up(sum, d);
-        if (lane >= d) sum += y;
-    }
-    return sum - x;
+// Sums over the lanes up to each one: six moves between lanes inside the vector
+// unit (through LDS a sum takes 0.2 us, of which a call has a dozen in a row).
+template <int CTRL, int ROWS>
+__device__ inline int moved(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false); }
+template <int CTRL, int ROWS>
+__device__ inline int64_t moved(int64_t x) {
+    return int64_t(uint64_t(uint32_t(moved<CTRL, ROWS>(int(x >> 32)))) << 32 | uint32_t(moved<CTRL, ROWS>(int(x))));
 }
-__device__ inline int over_lanes(int x) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
+template <typename T>
+__device__ inline T upto_lane(T x) {
+    x += moved<0x111, 0xf>(x);      // the lanes 1, 2, 4, 8 before, of 16
+    x += moved<0x112, 0xf>(x);
+    x += moved<0x114, 0xf>(x);
+    x += moved<0x118, 0xf>(x);
+    x += moved<0x142, 0xa>(x);      // the last one of the 16, and of the 32, before
+    x += moved<0x143, 0xc>(x);
     return x;
+}
+__device__ inline int of_lane(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
+__device__ inline int64_t of_lane(int64_t x, int lane) {
+    return int64_t(uint64_t(uint32_t(of_lane(int(x >> 32), lane))) << 32 | uint32_t(of_lane(int(x), lane)));
+}
+template <typename T>
+__device__ inline T over_lanes(T x) { return of_lane(upto_lane(x), 63); }
+
+// Sum of a list's first n, its loads in flight together.
+__device__ inline int64_t sum_of(const int32_t* list, int64_t n, int lane) {
+    int64_t sum = 0;
+    for (int64_t base = 0; base < n; base += 64 * 4) {
+        int x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = base + 64 * j + lane < n ? list[base + 64 * j + lane] : 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum += x[j];
+    }
+    return over_lanes(sum);
 }
 
 // LDS that a wave's lanes write for one another
@@ -57,29 +81,34 @@ __device__ inline void wave_sync() {
     __builtin_amdgcn_wave_barrier();
 }
 
-// Bits of the free pages and their number, block after block.
+// Bits of the free pages, and their number before each word of a block and in
+// it, block after block.
 __device__ inline void page_map(const PagesLaunch& a, const Crew& w, int64_t first_wave) {
     for (int64_t b = w.wave - first_wave; b < a.blocks; b += w.waves) {
         if (b < 0) continue;
         const int64_t base = b * kBlock;
         u64 mine = 0;
+        // sixteen words at a time, the next ones' loads under way; short code, which a call finds in no cache
+        int refs[16], next[16];
+        auto load = [&](int part, int (&to)[16]) {
 #pragma unroll
-        for (int part = 0; part < 4; ++part) {
-            int refs[16];
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                const int64_t page = base + (part * 16 + j) * 64 + w.lane;
-                refs[j] = a.refs[min(page, a.num_pages - 1)];
-            }
+            for (int j = 0; j < 16; ++j) to[j] = a.refs[min(base + (part * 16 + j) * 64 + w.lane, a.num_pages - 1)];
+        };
+        load(0, refs);
+#pragma unroll 1
+        for (int part = 0; part < 4 && base + part * 1024 < a.num_pages; ++part) {
+            load(part + 1, next);
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
                 const u64 bits = __ballot(refs[j] == 0 && base + (part * 16 + j) * 64 + w.lane < a.num_pages);
                 if (w.lane == part * 16 + j) mine = bits;
+                refs[j] = next[j];
             }
         }
+        const int n = __popcll(mine), upto = upto_lane(n);
         a.map[b * 64 + w.lane] = mine;
-        const int free = over_lanes(__popcll(mine));
-        if (w.lane == 0) a.free[b] = free;
+        a.before[b * 64 + w.lane] = upto - n;
+        if (w.lane == 63) a.free[b] = upto;
     }
 }
 
@@ -89,19 +118,19 @@ struct PageCursor {
     int64_t block;
     int64_t before;
 };
-__device__ inline int free_in(const PagesLaunch& a, int64_t b) { return b < a.blocks ? a.free[b] : 0; }
-// the first block with the r-th free page in it or before its end; blocks: there is none
+// the first block with the r-th free page in it; a.blocks: there is none
 __device__ inline void page_seek(const PagesLaunch& a, const Crew& w, int64_t r, PageCursor* c) {
     while (c->block < a.blocks) {
-        const int n = free_in(a, c->block + w.lane), upto = before_lane(n, w.lane) + n;
+        const int n = c->block + w.lane < a.blocks ? a.free[c->block + w.lane] : 0;
+        const int64_t upto = upto_lane(int64_t(n));
         const u64 past = __ballot(c->before + upto > r);
         if (past) {
             const int at = __builtin_ctzll(past);
-            c->before += __shfl(upto - n, at);
+            c->before += of_lane(upto - n, at);
             c->block += at;
             return;
         }
-        c->before += __shfl(upto, 63);
+        c->before += of_lane(upto, 63);
         c->block += 64;
     }
     c->block = a.blocks;
@@ -113,31 +142,17 @@ __device__ inline int page_take(const PagesLaunch& a, const Crew& w, int64_t r, 
         page_seek(a, w, r + got, c);
         if (c->block >= a.blocks) break;
         u64 bits = a.map[c->block * 64 + w.lane];
-        const int n = __popcll(bits), at = before_lane(n, w.lane);
-        int64_t rank = c->before + at;
+        const int n = __popcll(bits);
+        int64_t rank = c->before + a.before[c->block * 64 + w.lane];
         const int64_t end = r + count;
         if (rank < end && rank + n > r) {
             for (; bits; bits &= bits - 1, ++rank)
                 if (rank >= r && rank < end) to[rank - r] = int32_t(c->block * kBlock + w.lane * 64 + __builtin_ctzll(bits));
         }
-        const int64_t block_end = c->before + over_lanes(n);
-        got = int(min(end, block_end) - r);
+        got = int(min(end, c->before + a.free[c->block]) - r);
     }
     wave_sync();
     return got;
-}
-__device__ inline int64_t all_free(const PagesLaunch& a, const Crew& w) {
-    int sum = 0;
-    for (int64_t b = w.lane; b < a.blocks; b += 64) sum += a.free[b];
-    return over_lanes(sum);
-}
-// the wants of the sequences before i
-__device__ inline int64_t wants_before(const PagesLaunch& a, const Crew& w, int64_t i) {
-    int64_t sum = 0;
-    for (int64_t j = w.lane; j < i; j += 64) sum += a.want[j];
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor((long long)sum, d);
-    return sum;
 }
 
 __device__ inline int pages_of(const PagesLaunch& a, int len) { return int(min(a.max_pages, (int64_t(max(len, 0)) + (1 << a.log2_page) - 1) >> a.log2_page)); }
@@ -154,12 +169,12 @@ __device__ void grow_count(const PagesLaunch& a, const Crew& w) {
         const int32_t* row = row_of(a, a.rows[i]);
         const int need = row ? pages_of(a, a.lens[i]) : 0;
         int count = 0, first = need;
-        for (int base = 0; base < need; base += 64 * 8) {
-            int page[8];
+        for (int base = 0; base < need; base += 64 * 4) {
+            int page[4];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) page[j] = row[min(base + 64 * j + w.lane, need - 1)];
+            for (int j = 0; j < 4; ++j) page[j] = row[min(base + 64 * j + w.lane, need - 1)];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < 4; ++j) {
                 const u64 none = __ballot(page[j] < 0 && base + 64 * j + w.lane < need);
                 if (none && first == need) first = base + 64 * j + __builtin_ctzll(none);
                 count += __popcll(none);
@@ -173,9 +188,9 @@ __device__ void grow_give(const PagesLaunch& a, const Crew& w, int32_t* pages) {
     for (int64_t i = w.wave; i < max(a.n, int64_t(1)); i += w.waves) {
         const int want = a.n ? a.want[i] : 0;
         if (want == 0 && i < a.n - 1) continue;
-        int64_t rank = wants_before(a, w, i);
+        int64_t rank = sum_of(a.want, i, w.lane);
         if (i >= a.n - 1) {                                 // the last one knows them all
-            const int64_t missing = rank + want - all_free(a, w);
+            const int64_t missing = rank + want - sum_of(a.free, a.blocks, w.lane);
             if (w.lane == 0) *a.count = int32_t(max(int64_t(0), missing));
         }
         if (want == 0) continue;
@@ -210,46 +225,53 @@ __device__ void fork_count(const PagesLaunch& a, const Crew& w) {
 __device__ void fork_give(const PagesLaunch& a, const Crew& w, int32_t* pages) {
     for (int64_t i = w.wave; i < max(a.n, int64_t(1)); i += w.waves) {
         const int want = a.n ? a.want[i] : 0;
+        const int32_t* from = a.n ? row_of(a, a.parents[i]) : nullptr;
+        int32_t* to = a.n ? row_of(a, a.rows[i]) : nullptr;
+        const int64_t len = from ? min(int64_t(max(a.lens[i], 0)), a.max_pages << a.log2_page) : 0;
+        const int full = int(len >> a.log2_page), part = int(len & ((1 << a.log2_page) - 1));
+        // the parent's entries are on their way while the child's own page is found
+        int page[8], old = want ? from[full] : -1;
+        auto load = [&](int64_t base) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int64_t at = base + 64 * j + w.lane;
+                page[j] = at < full ? from[at] : -1;
+            }
+        };
+        load(0);
         const bool last = i >= a.n - 1;
-        const int64_t rank = want || last ? wants_before(a, w, i) : 0;
+        const int64_t rank = want || last ? sum_of(a.want, i, w.lane) : 0;
         if (last) {
-            const int64_t all = rank + want, free = all_free(a, w), pairs = min(all, free);
+            const int64_t all = rank + want, pairs = min(all, sum_of(a.free, a.blocks, w.lane));
             if (w.lane == 0) a.count[0] = int32_t(pairs), a.count[1] = int32_t(all - pairs);
             for (int64_t j = pairs + w.lane; j < a.n; j += 64) a.src[j] = a.dst[j] = a.tokens[j] = -1;
-            if (a.n == 0) continue;
         }
-        const int32_t* from = row_of(a, a.parents[i]);
-        int32_t* to = row_of(a, a.rows[i]);
         if (!to) continue;
-        const int64_t len = from ? min(int64_t(max(a.lens[i], 0)), a.max_pages << a.log2_page) : 0;
-        const int full = int(len >> a.log2_page);
         int own = -1;
         if (want) {
             PageCursor c{0, 0};
             if (page_take(a, w, rank, 1, &c, pages)) own = pages[0];
             wave_sync();
             if (own >= 0 && w.lane == 0) {
-                a.src[rank] = from[full];
+                a.src[rank] = old;
                 a.dst[rank] = own;
-                a.tokens[rank] = int32_t(len & ((1 << a.log2_page) - 1));
+                a.tokens[rank] = part;
                 atomicAdd(&a.refs[own], 1);
             }
         }
-        for (int64_t base = 0; base < a.max_pages; base += 64 * 4) {
-            int page[4];
+        for (int64_t base = 0; base < a.max_pages; base += 64 * 8) {
+            if (base) load(base);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < 8; ++j) {
                 const int64_t at = base + 64 * j + w.lane;
-                page[j] = at < full ? from[at] : at == full ? own : -1;
+                if (at >= a.max_pages) break;
+                const bool shared = at < full && is_page(a, page[j]);
+                if (shared) atomicAdd(&a.refs[page[j]], 1);
+                page[j] = atomicExch(&to[at], shared ? page[j] : at == full ? own : -1);
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int64_t at = base + 64 * j + w.lane;
-                if (at >= a.max_pages) continue;
-                const int page_here = is_page(a, page[j]) ? page[j] : -1;
-                if (at < full && page_here >= 0) atomicAdd(&a.refs[page_here], 1);
-                let_go(a, atomicExch(&to[at], page_here));
-            }
+            for (int j = 0; j < 8; ++j)
+                if (base + 64 * j + w.lane < a.max_pages) let_go(a, page[j]);
         }
     }
 }
@@ -257,53 +279,35 @@ __device__ void fork_give(const PagesLaunch& a, const Crew& w, int32_t* pages) {
 // compact, second phase: of U pages in use, the M that lie behind the first U
 // pages, from the last one on, go to the free ones among those, from the first
 // one on.  With f(p) free pages before p, page p is the (U - 1 - (p - f(p)))-th
-// in use from the end.
-struct CompactSizes {
-    int64_t used, moves;
-};
-__device__ inline CompactSizes compact_sizes(const PagesLaunch& a, const Crew& w) {
-    CompactSizes s;
-    s.used = a.num_pages - all_free(a, w);
-    const int64_t block = s.used / kBlock;      // of page U
-    int64_t before = 0;
-    for (int64_t b = w.lane; b < min(block, a.blocks); b += 64) before += a.free[b];
-    if (block < a.blocks) {
-        const int64_t left = s.used - block * kBlock - w.lane * 64;     // pages of this lane's word before page U
-        const u64 bits = a.map[block * 64 + w.lane] & (left <= 0 ? 0 : left >= 64 ? ~0ull : (1ull << left) - 1);
-        before += __popcll(bits);
-    }
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) before += __shfl_xor((long long)before, d);
-    s.moves = min(before, a.n);
-    return s;
-}
+// in use from the end.  A wave takes a quarter of a block, a page a lane; what
+// it leaves in 'before' counts from the first page on.
 __device__ void compact_list(const PagesLaunch& a, const Crew& w) {
-    if (w.wave >= a.blocks && w.wave > 0) return;
-    const CompactSizes s = compact_sizes(a, w);
-    if (w.wave == 0 && w.lane == 0) a.count[0] = int32_t(s.moves), a.count[1] = int32_t(s.used);
-    const int64_t crew = min(w.waves, a.blocks);
-    for (int64_t k = s.moves + w.wave * 64 + w.lane; k < a.n; k += crew * 64) a.src[k] = a.dst[k] = -1;
-    int64_t before_block = 0, at = 0;
-    for (int64_t b = w.wave; b < a.blocks; b += w.waves) {
-        int64_t sum = 0;
-        for (int64_t j = at + w.lane; j < b; j += 64) sum += a.free[j];
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) sum += __shfl_xor((long long)sum, d);
-        before_block += sum;
-        at = b;
-        const u64 mine = a.map[b * 64 + w.lane];
-        const int before = before_lane(__popcll(mine), w.lane);
-        // word after word, a page a lane
-        for (int j = 0; j < 64 && b * kBlock + j * 64 < a.num_pages; ++j) {
-            const u64 bits = __shfl((long long)mine, j);
-            const int64_t page = b * kBlock + j * 64 + w.lane, f = before_block + __shfl(before, j) + __popcll(bits & ((1ull << w.lane) - 1));
-            if (page >= a.num_pages) continue;
-            const bool free = bits >> w.lane & 1;
-            if (free && page < s.used && f < s.moves) a.dst[f] = int32_t(page);
-            const int64_t k = s.used - 1 - (page - f);
-            if (!free && page >= s.used) {
-                a.name[page] = int32_t(k < s.moves ? k : -1);
-                if (k < s.moves) a.src[k] = int32_t(page);
+    const int64_t used = a.num_pages - sum_of(a.free, a.blocks, w.lane), at_used = used / kBlock;   // the block of page U
+    const int64_t before_used = sum_of(a.free, min(at_used, a.blocks), w.lane);
+    int rest = 0;
+    if (at_used < a.blocks) {
+        const int64_t left = used - at_used * kBlock - w.lane * 64;     // pages of this lane's word before page U
+        rest = __popcll(a.map[at_used * 64 + w.lane] & (left <= 0 ? 0 : left >= 64 ? ~0ull : (1ull << left) - 1));
+    }
+    const int64_t moves = min(before_used + over_lanes(rest), a.n);
+    if (w.wave == 0 && w.lane == 0) a.count[0] = int32_t(moves), a.count[1] = int32_t(used);
+    for (int64_t k = moves + w.wave * 64 + w.lane; k < a.n; k += w.waves * 64) a.src[k] = a.dst[k] = -1;
+    for (int64_t item = w.wave; item < a.blocks * 4; item += w.waves) {
+        // a word a lane, the numbers before them counted from the first page on
+        const int64_t mine = item * 16 + (w.lane & 15);
+        const u64 word = a.map[mine];
+        const int before = int(sum_of(a.free, item / 4, w.lane)) + a.before[mine];
+        wave_sync();
+        if (w.lane < 16) a.before[mine] = before;
+#pragma unroll 1
+        for (int j = 0; j < 16 && (item * 16 + j) * 64 < a.num_pages; ++j) {
+            const u64 bits = u64(of_lane(int64_t(word), j));
+            const int64_t page = (item * 16 + j) * 64 + w.lane, f = of_lane(before, j) + __popcll(bits & ((1ull << w.lane) - 1));
+            const int64_t k = used - 1 - (page - f);
+            if (bits >> w.lane & 1) {
+                if (page < used && f < moves) a.dst[f] = int32_t(page);
+            } else if (page >= used && page < a.num_pages && k < moves) {
+                a.src[k] = int32_t(page);
             }
         }
     }
@@ -311,16 +315,20 @@ __device__ void compact_list(const PagesLaunch& a, const Crew& w) {
 // third phase: references and tables follow
 __device__ void compact_apply(const PagesLaunch& a, const Crew& w) {
     const int64_t moves = a.count[0], used = a.count[1], thread = w.wave * 64 + w.lane, threads = w.waves * 64;
+#pragma unroll 1
     for (int64_t k = thread; k < moves; k += threads) {
-        a.refs[a.dst[k]] = a.refs[a.src[k]];
-        a.refs[a.src[k]] = 0;
+        const int src = a.src[k], dst = a.dst[k];
+        a.refs[dst] = a.refs[src];
+        a.refs[src] = 0;
     }
     const int64_t entries = int64_t(a.num_rows) * a.max_pages;
+#pragma unroll 1
     for (int64_t i = thread; i < entries; i += threads) {
         const int page = a.table[i];
-        if (page < used || page >= a.num_pages || a.map[page / 64] >> (page % 64) & 1) continue;
-        const int k = a.name[page];
-        if (k >= 0) a.table[i] = a.dst[k];
+        if (page < used || page >= a.num_pages) continue;
+        const u64 bits = a.map[page / 64], bit = 1ull << (page % 64);
+        const int64_t k = used - 1 - (page - (a.before[page / 64] + __popcll(bits & (bit - 1))));
+        if (!(bits & bit) && k < moves) a.table[i] = a.dst[k];
     }
 }
 
@@ -330,11 +338,14 @@ __device__ inline void next_phase() {
     __syncthreads();
 }
 
-template <int OP, int PHASE>       // PHASE 0: all of them
+template <int OP, int PHASE>       // PHASE 0: all of them, whose notes to one another stay in LDS
 __global__ __launch_bounds__(PHASE ? kThreads : kWide) void pages_kernel(PagesLaunch a) {
     __shared__ int32_t pages_s[(PHASE ? kThreads : kWide) / 64][64];
+    __shared__ u64 map_s[PHASE ? 1 : kFewBlocks * 64];
+    __shared__ int32_t before_s[PHASE ? 1 : kFewBlocks * 64], free_s[PHASE ? 1 : kFewBlocks], want_s[PHASE ? 1 : kFewRows], first_s[PHASE ? 1 : kFewRows];
     const Crew w = crew();
     int32_t* pages = pages_s[threadIdx.x / 64];
+    if (PHASE == 0) a.map = map_s, a.before = before_s, a.free = free_s, a.want = want_s, a.first = first_s;
     if (PHASE <= 1) {
         if (OP == kPagesGrow) grow_count(a, w);
         if (OP == kPagesFork) fork_count(a, w);
@@ -346,7 +357,7 @@ __global__ __launch_bounds__(PHASE ? kThreads : kWide) void pages_kernel(PagesLa
         if (OP == kPagesFork) fork_give(a, w, pages);
         if (OP == kPagesCompact) compact_list(a, w);
     }
-    if (PHASE == 0) next_phase();
+    if (PHASE == 0 && OP == kPagesCompact) next_phase();
     if ((PHASE == 0 || PHASE == 3) && OP == kPagesCompact) compact_apply(a, w);
 }
 
@@ -358,8 +369,7 @@ __global__ __launch_bounds__(kThreads) void pages_free_kernel(PagesLaunch a, int
     int32_t* row = row_of(a, a.rows[i]);
     if (!row) return;
     const int64_t at = (a.lens ? pages_of(a, a.lens[i]) : 0) + (w.wave - i * parts) * 64 + w.lane;
-    for (int64_t j = at; j < a.max_pages; j += int64_t(parts) * 64)
-        if (row[j] != -1) let_go(a, atomicExch(&row[j], -1));
+    for (int64_t j = at; j < a.max_pages; j += int64_t(parts) * 64) let_go(a, atomicExch(&row[j], -1));
 }
 
 // ---------------------------------------------------------------------------
@@ -407,7 +417,7 @@ template <int OP>
 hipError_t launch_phases(const PagesLaunch& given, int64_t first, int64_t second, int64_t third, hipStream_t stream) {
     PagesLaunch a = given;
     // one workgroup of sixteen waves where none has more than a few things to do
-    if (first + a.blocks <= 64 && second <= 64 && third <= 512) {
+    if (a.blocks <= kFewBlocks && second <= kFewRows && third <= 64) {
         hipLaunchKernelGGL((pages_kernel<OP, 0>), dim3(1), dim3(kWide), 0, stream, a);
         return hipGetLastError();
     }
@@ -427,12 +437,12 @@ hipError_t launch_phases(const PagesLaunch& given, int64_t first, int64_t second
 hipError_t launch_pages_grow(const PagesLaunch& a, hipStream_t stream) { return launch_phases<kPagesGrow>(a, a.n, a.n, 0, stream); }
 hipError_t launch_pages_fork(const PagesLaunch& a, hipStream_t stream) { return launch_phases<kPagesFork>(a, (a.n + 63) / 64, a.n, 0, stream); }
 hipError_t launch_pages_compact(const PagesLaunch& a, hipStream_t stream) {
-    return launch_phases<kPagesCompact>(a, 0, a.blocks, std::max((int64_t(a.num_rows) * a.max_pages + 63) / 64, (a.n + 63) / 64), stream);
+    return launch_phases<kPagesCompact>(a, 0, a.blocks * 4, std::max((int64_t(a.num_rows) * a.max_pages + 63) / 64, (a.n + 63) / 64), stream);
 }
 
 hipError_t launch_pages_free(const PagesLaunch& a, hipStream_t stream) {
-    // entries of a row for a wave: 256, and more than that only where the launch would be too large
-    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>((a.max_pages + 255) / 256, (int64_t(1) << 22) / a.n));
+    // entries of a row for a wave: 64, and more than that only where the launch would be too large
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>((a.max_pages + 63) / 64, (int64_t(1) << 22) / a.n));
     hipLaunchKernelGGL(pages_free_kernel, dim3(groups_of(a.n * parts)), dim3(kThreads), 0, stream, a, int(parts));
     return hipGetLastError();
 }

@@ -95,17 +95,15 @@ bool hits(const tl_kv_pages* p, int64_t n, std::initializer_list<const int32_t*>
     return false;
 }
 
-// The workspace of n sequences and the names of 'names' pages.
-int pages_workspace(PagesLaunch* a, int64_t n, int64_t names, StreamHold* hold, void* stream) {
-    const int64_t words = (a->blocks + 3) / 4 * 4, list = (n + 3) / 4 * 4;
+int pages_workspace(PagesLaunch* a, int64_t n, StreamHold* hold, void* stream) {
     void* ws = nullptr;
-    const int st = stream_workspace((hipStream_t)stream, size_t(a->blocks * 512 + (words + 2 * list + names) * 4), hold, &ws);
+    const int st = stream_workspace((hipStream_t)stream, size_t(a->blocks * (64 * 12 + 4) + n * 8), hold, &ws);
     if (st != TL_OK) return st;
     a->map = static_cast<unsigned long long*>(ws);
-    a->free = reinterpret_cast<int32_t*>(a->map + a->blocks * 64);
-    a->want = a->free + words;
-    a->first = a->want + list;
-    a->name = a->first + list;
+    a->before = reinterpret_cast<int32_t*>(a->map + a->blocks * 64);
+    a->free = a->before + a->blocks * 64;
+    a->want = a->free + a->blocks;
+    a->first = a->want + n;
     return TL_OK;
 }
 
@@ -266,7 +264,7 @@ int tl_kv_grow(const tl_kv_pages* pages, const int32_t* rows, const int32_t* len
     a.lens = lens;
     a.count = missing;
     StreamHold hold;
-    const int st = pages_workspace(&a, n, 0, &hold, stream);
+    const int st = pages_workspace(&a, n, &hold, stream);
     return st != TL_OK ? st : done(launch_pages_grow(a, (hipStream_t)stream));
 }
 
@@ -296,7 +294,7 @@ int tl_kv_fork(const tl_kv_pages* pages, const int32_t* parents, const int32_t* 
     a.tokens = tokens;
     a.count = count;
     StreamHold hold;
-    const int st = pages_workspace(&a, n, 0, &hold, stream);
+    const int st = pages_workspace(&a, n, &hold, stream);
     return st != TL_OK ? st : done(launch_pages_fork(a, (hipStream_t)stream));
 }
 
@@ -312,7 +310,7 @@ int tl_kv_compact(const tl_kv_pages* pages, int64_t max_moves, int32_t* src, int
     a.dst = dst;
     a.count = count;
     StreamHold hold;
-    const int st = pages_workspace(&a, 0, a.num_pages, &hold, stream);
+    const int st = pages_workspace(&a, 0, &hold, stream);
     return st != TL_OK ? st : done(launch_pages_compact(a, (hipStream_t)stream));
 }
 

@@ -137,15 +137,15 @@ struct PagesLaunch {
     int32_t* dst;
     int32_t* tokens;
     int32_t* count;             // grow: missing
-    // workspace: bits of the free pages and their number per block of pages; of
-    // each sequence the pages that it wants, and the first entry without one;
-    // of each page its place in the list of moves
+    // workspace: bits of the free pages, and their number before each word of a
+    // block of pages and in the block; of each sequence the pages that it wants,
+    // and the first entry without one
     int64_t blocks;
     unsigned long long* map;
+    int32_t* before;
     int32_t* free;
     int32_t* want;
     int32_t* first;
-    int32_t* name;
     int64_t map_wave;           // the first wave of a launch that makes bits
 };
 hipError_t launch_pages_grow(const PagesLaunch& a, hipStream_t stream);
