@@ -53,9 +53,19 @@ __device__ inline int64_t uniform(int64_t x) {
     return int64_t(uint64_t(uint32_t(uniform(int(x >> 32)))) << 32 | uint32_t(uniform(int(x))));
 }
 
-// a / b of a >= 0, b > 0 below 2^53 by way of a double: a sixth of the
-// instructions of a 64-bit integer division
+// a / b of a >= 0, b > 0 below 2^53.  A workgroup makes six such divisions in a row
+// before its first load.  Below 2^31: by way of a float's reciprocal, off by at
+// most 2^-21 of itself, and of that of what is left (below 2^10 b, so that the
+// second is off by less than one): 20 instructions; else by way of a double, 50,
+// and a sixth of a 64-bit integer division's.
 __device__ inline int64_t quotient(int64_t a, int64_t b) {
+    if (uint64_t(a) < 0x80000000u && uint64_t(b) < 0x80000000u) {
+        const float inv = __builtin_amdgcn_rcpf(float(int(b)));
+        int q = int(float(int(a)) * inv);
+        q += int(float(int(uint32_t(a) - uint32_t(q) * uint32_t(b))) * inv);
+        const int r = int(uint32_t(a) - uint32_t(q) * uint32_t(b));
+        return q + (r >= int(b)) - (r < 0);
+    }
     const int64_t q = int64_t(double(a) / double(b)), r = a - q * b;
     return q + (r >= b) - (r < 0);
 }
@@ -103,12 +113,7 @@ __device__ inline Seq attn_scan(const AttnLaunch& a, int base, int64_t* upto) {
         s.len = int(max(int64_t(0), min(int64_t(len), min(a.max_pages << a.c.log2_page, a.max_len))));
         attn_sizes(a, &s);
     }
-    *upto = b < a.num_seqs ? attn_places(a, s) : 0;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int64_t x = __shfl_up((long long)*upto, d);
-        if (lane >= d) *upto += x;
-    }
+    *upto = upto_lane(b < a.num_seqs ? attn_places(a, s) : 0);
     return s;
 }
 
@@ -124,7 +129,7 @@ __device__ inline int64_t attn_total(const AttnLaunch& a, AttnLine* line) {
             line->len[lane] = s.len;
             line->upto[lane] = upto;
         }
-        before += uniform(int64_t(__shfl((long long)upto, 63)));
+        before += of_lane(upto, 63);
     }
     return before;
 }
@@ -149,13 +154,13 @@ __device__ inline Seq attn_find(const AttnLaunch& a, const AttnLine* line, int64
             if (past) {
                 const int who = uniform(__builtin_ctzll(past));
                 s.seq = base + who;
-                s.first = uniform(__shfl(x.first, who));
-                s.n = uniform(__shfl(x.n, who));
-                s.len = uniform(__shfl(x.len, who));
-                s.before = before + (who ? uniform(int64_t(__shfl((long long)upto, who - 1))) : 0);
+                s.first = of_lane(x.first, who);
+                s.n = of_lane(x.n, who);
+                s.len = of_lane(x.len, who);
+                s.before = before + (who ? of_lane(upto, who - 1) : 0);
                 break;
             }
-            before += uniform(int64_t(__shfl((long long)upto, 63)));
+            before += of_lane(upto, 63);
         }
     }
     attn_sizes(a, &s);

@@ -44,4 +44,29 @@ __device__ inline u32x4 fp4_to_bf16x8(uint32_t w, float scale) {
 // 2^(e - 127) of a biased exponent
 __device__ inline float exp_scale(uint32_t e) { return __uint_as_float(e << 23); }
 
+// Sums over the lanes up to each one: six moves between lanes inside the vector
+// unit (through LDS each takes about 60 ns more, one after the other).
+template <int CTRL, int ROWS>
+__device__ inline int moved(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false); }
+template <int CTRL, int ROWS>
+__device__ inline int64_t moved(int64_t x) {
+    return int64_t(uint64_t(uint32_t(moved<CTRL, ROWS>(int(x >> 32)))) << 32 | uint32_t(moved<CTRL, ROWS>(int(x))));
+}
+template <typename T>
+__device__ inline T upto_lane(T x) {
+    x += moved<0x111, 0xf>(x);      // the lanes 1, 2, 4, 8 before, of 16
+    x += moved<0x112, 0xf>(x);
+    x += moved<0x114, 0xf>(x);
+    x += moved<0x118, 0xf>(x);
+    x += moved<0x142, 0xa>(x);      // the last one of the 16, and of the 32, before
+    x += moved<0x143, 0xc>(x);
+    return x;
+}
+__device__ inline int of_lane(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
+__device__ inline int64_t of_lane(int64_t x, int lane) {
+    return int64_t(uint64_t(uint32_t(of_lane(int(x >> 32), lane))) << 32 | uint32_t(of_lane(int(x), lane)));
+}
+template <typename T>
+__device__ inline T over_lanes(T x) { return of_lane(upto_lane(x), 63); }
+
 }  // namespace tl
