@@ -26,7 +26,7 @@ __device__ inline void wait_for_lds_loads() {
 
 // The work is a line: sequence after sequence, in it head after head, in it
 // tile after tile of rows.  Without a split a workgroup takes one tile of a
-// head.  With one, a tile takes as many places as it costs, in sixteenths of a
+// head (sorted: the longest of all first).  With one, a tile takes as many places as it costs, in sixteenths of a
 // chunk of keys: its chunks and kTileCost for its start and end, a causal
 // tile's chunks rising evenly from one tile to the next.  Workgroup w of W
 // takes the places [w T / W, (w + 1) T / W) of all T and of each tile the
@@ -225,7 +225,8 @@ __device__ inline bool attn_begin(const AttnLaunch& a, AttnLine* line, AttnRun* 
         r->end = uniform(quotient((r->me + 1) * r->total, r->groups));
     } else {
         if (r->me >= r->total) return false;
-        r->place = r->me = attn_by_xcd(r->me, int(r->total));
+        if (!a.sorted) r->me = attn_by_xcd(r->me, int(r->total));
+        r->place = r->me;
         r->end = r->place + 1;
     }
     r->place0 = r->place;
@@ -239,16 +240,61 @@ struct AttnPiece {
     bool whole;
     int64_t slot;       // of its partial result, if it is not the whole tile
 };
+
+// The tile at place p where the longest ones come first: sequence (one a lane),
+// head and tile.  Tiles of a sequence grow with their number, so that those of
+// more than k chunks are its last ones, of a number in closed form; k is found by
+// bisection of the sum over sequences.
+__device__ inline void attn_sorted(const AttnLaunch& a, const AttnLine* line, int64_t p, AttnPiece* piece) {
+    const int lane = threadIdx.x & 63;
+    Seq s{};
+    if (lane < a.num_seqs) {
+        s.n = line->n[lane];
+        s.len = line->len[lane];
+        attn_sizes(a, &s);
+    }
+    const int start = s.len - s.n, rows = 1 << a.log2_rows;
+    // tiles of the lane's sequence that have more than k chunks
+    auto longer = [&](int k) {
+        const int64_t keys = int64_t(k) << a.log2_keys;
+        if (keys >= (a.mask ? s.len : min(s.len, start + s.rows))) return 0;
+        if (a.mask || keys <= start) return s.tiles;
+        return s.tiles - (int(((keys - start) * a.group + rows) >> a.log2_rows) - 1);      // the first whose last row's token is keys - start or later
+    };
+    auto all_longer = [&](int k) { return over_lanes(int64_t(longer(k))) * a.c.heads; };
+    int most = s.tiles ? (s.len + (1 << a.log2_keys) - 1) >> a.log2_keys : 0;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) most = max(most, __shfl_xor(most, d));
+    int lo = 0, hi = uniform(most);                // none has more than hi
+    while (lo < hi) {
+        const int k = (lo + hi) / 2;
+        if (all_longer(k) <= p) hi = k;
+        else lo = k + 1;
+    }
+    // of those of lo chunks the item-th
+    const int64_t left = p - all_longer(lo);
+    const int item = uniform(int(quotient(left, a.c.heads)));
+    const int after = longer(lo), mine = (lo ? longer(lo - 1) : s.tiles) - after, upto = upto_lane(mine);
+    const int who = uniform(__builtin_ctzll(__ballot(upto > item) | 1ull << 63));
+    piece->s.seq = who;
+    piece->s.first = uniform(line->first[who]);
+    piece->s.n = uniform(line->n[who]);
+    piece->s.len = uniform(line->len[who]);
+    attn_sizes(a, &piece->s);
+    piece->head = uniform(int(left - int64_t(item) * a.c.heads));
+    piece->tile = piece->s.tiles - 1 - of_lane(after, who) - (item - of_lane(upto - mine, who));
+}
 template <int D>
 __device__ inline AttnPiece attn_piece(const AttnLaunch& a, const AttnLine* line, AttnRun* r) {
     AttnPiece p;
-    p.s = attn_find(a, line, r->place);
+    if (a.sorted) attn_sorted(a, line, r->place, &p);
+    else p.s = attn_find(a, line, r->place);
     const int64_t in_seq = r->place - p.s.before;
     if (a.split) {
         const int64_t per_head = attn_cost(p.s, p.s.tiles);
         p.head = uniform(int(quotient(in_seq, per_head)));
         p.tile = uniform(attn_tile_at(p.s, in_seq - p.head * per_head));
-    } else {
+    } else if (!a.sorted) {
         p.head = uniform(int(quotient(in_seq, p.s.tiles)));
         p.tile = p.s.tiles - 1 - uniform(int(in_seq - int64_t(p.head) * p.s.tiles));    // the longest first
     }

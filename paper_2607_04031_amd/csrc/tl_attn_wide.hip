@@ -100,10 +100,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
         }
         f32x4v o[kRowTiles][D / 16];
         float m[kRowTiles], l[kRowTiles];
+        f32x4v ones_sum[kRowTiles];     // 4 bits: the rounded weights' sums, by a product with ones (any element)
 #pragma unroll
         for (int nt = 0; nt < kRowTiles; ++nt) {
             m[nt] = -INFINITY;
             l[nt] = 0.f;
+            ones_sum[nt] = f32x4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int db = 0; db < D / 16; ++db) o[nt][db] = f32x4v{0.f, 0.f, 0.f, 0.f};
         }
@@ -280,8 +282,46 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
             }
             // running maximum and sum, as in attn_kernel
             u32x4 p[kRowTiles][2];
+            if (kFour) {
+                // both row tiles together: the one's instructions run while the other's results are on their way
+                float top[kRowTiles];
+                bool grows = false;
 #pragma unroll
-            for (int nt = 0; nt < kRowTiles; ++nt) {
+                for (int nt = 0; nt < kRowTiles; ++nt) {
+                    top[nt] = -INFINITY;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) top[nt] = fmaxf(top[nt], x[nt][e >> 2][e & 3]);
+                    grows |= top[nt] * a.scale_log2 > m[nt] + kSlack;
+                }
+                if (__ballot(grows)) {
+#pragma unroll
+                    for (int nt = 0; nt < kRowTiles; ++nt) {
+                        top[nt] = fmaxf(top[nt], __shfl_xor(top[nt], 16));
+                        top[nt] = fmaxf(top[nt], __shfl_xor(top[nt], 32));
+                        const float grown = fmaxf(m[nt], top[nt] * a.scale_log2);
+                        const float shrink = __builtin_amdgcn_exp2f(m[nt] - (grown == -INFINITY ? 0.f : grown));
+                        m[nt] = grown;
+                        ones_sum[nt] *= shrink;
+#pragma unroll
+                        for (int db = 0; db < D / 16; ++db) o[nt][db] *= shrink;
+                    }
+                }
+                float base[kRowTiles];
+#pragma unroll
+                for (int nt = 0; nt < kRowTiles; ++nt) base[nt] = m[nt] == -INFINITY ? 0.f : m[nt];
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2)
+#pragma unroll
+                        for (int nt = 0; nt < kRowTiles; ++nt) {
+                            const f32x4v& z = x[nt][2 * h + (e >> 2)];
+                            p[nt][h][e / 2] = pack_bf16(__builtin_amdgcn_exp2f(__builtin_fmaf(z[e & 3], a.scale_log2, -base[nt])),
+                                                        __builtin_amdgcn_exp2f(__builtin_fmaf(z[(e & 3) + 1], a.scale_log2, -base[nt])));
+                        }
+            }
+#pragma unroll
+            for (int nt = 0; nt < (kFour ? 0 : kRowTiles); ++nt) {
                 float top = -INFINITY;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) top = fmaxf(top, x[nt][e >> 2][e & 3]);
@@ -328,6 +368,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int nt = 0; nt < kRowTiles; ++nt) o[nt][2 * t + i / 2] = mfma_16x16x32(vf[t & 1][i], p[nt][i & 1], o[nt][2 * t + i / 2]);
+                if (kFour && t < 2) {
+#pragma unroll
+                    for (int nt = 0; nt < kRowTiles; ++nt) ones_sum[nt] = mfma_16x16x32(u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u}, p[nt][t & 1], ones_sum[nt]);
+                }
             }
             __builtin_amdgcn_s_setprio(0);
             __builtin_amdgcn_sched_barrier(0);
@@ -389,6 +433,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
         for (int nt = 0; nt < kRowTiles; ++nt) {
             l[nt] += __shfl_xor(l[nt], 16);
             l[nt] += __shfl_xor(l[nt], 32);
+            if (kFour) l[nt] = ones_sum[nt][0];
 #pragma unroll
             for (int db = 0; db < D / 16; ++db) *reinterpret_cast<f32x4v*>(mine + col2 * kPad + db * 16 + 4 * g2) = o[nt][db];
             __builtin_amdgcn_wave_barrier();

@@ -121,7 +121,14 @@ int pages_workspace(PagesLaunch* a, int64_t n, StreamHold* hold, void* stream) {
 //     two tiles to a slot, which trees need (64 of 32 nodes over 2048 tokens 128
 //     and 121, 16-bit 135 and 117), and prompts, whose tiles differ, do not (8 of
 //     512 tokens 148 and 167);
-//   - where each gets four tiles.
+//   - where each gets four tiles;
+//   - prompts over a 4-bit cache with a tile for every slot: whole tiles, the
+//     longest of all first, since a slot that is free takes the next one.  Three
+//     prompts of 2048 over 4096 (1180 tiles) 172 and 146, two of 2048 (1392) 125
+//     and 98, six of 1024 (764) 67 and 47, one of 2048 (512) 77 and 63; of equal
+//     length, 544 over 1088 (544) 67 and 53, over 8192 319 and 380, which is why
+//     fewer than two tiles a slot have to be short or of different lengths (1088
+//     over 8192 533 and 581, 1024 500 and 473, 1280 622 and 594).
 // All of it goes by max_len, the caller's bound: one far above the lengths splits
 // what need not be.
 int64_t plan_attn(AttnLaunch* a, int head_dim, int elem_bytes) {
@@ -138,6 +145,9 @@ int64_t plan_attn(AttnLaunch* a, int head_dim, int elem_bytes) {
     const int64_t whole = rows > 16 ? 1024 : elem_bytes != 2 ? 2048 : 1536;
     const bool enough = wide ? a->mask && a->max_tiles >= 2 * kSlots && a->max_len <= 2048 : a->max_tiles >= kSlots && a->max_len <= 4096;
     a->split = a->max_len > whole && !enough && a->max_tiles < 4 * kSlots;
+    a->sorted = elem_bytes == TL_KV_E2M1 && wide && !a->mask && a->num_seqs <= 64 && a->max_tiles >= kSlots &&
+                (a->max_len <= 4096 || 2 * a->max_q >= a->max_len || a->max_tiles >= 2 * kSlots);
+    if (a->sorted) a->split = false;
     a->groups = int(a->split ? kSlots : a->max_tiles);
     return a->split ? 2 * a->groups * rows * (head_dim + 2) + a->groups * 8 : 0;
 }

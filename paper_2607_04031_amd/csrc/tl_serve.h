@@ -189,6 +189,7 @@ struct AttnLaunch {
     // workgroups, and how many of those
     int log2_rows, log2_keys;
     bool split;
+    bool sorted;              // not split, at most 64 sequences: the longest tiles of all first
     int64_t max_tiles;
     int groups;
     float* ws;                // partial results: two per workgroup (split)

@@ -246,3 +246,28 @@ def test_cache_past_four_gigabytes():
     want, size = _serve.attention(q, small, [[0, 1, 2]], [L], [0, 1], D ** -0.5)
     got = out.cpu().double().numpy()
     _near(got, want, size)
+
+
+@pytest.mark.parametrize("D,G", [(128, 3), (64, 3), (128, 20)])
+def test_prompts_with_a_tile_for_every_workgroup(D, G):
+    """Whole tiles, the longest of all sequences and heads first: ragged lengths, among them none and fewer keys than rows, and
+    a bound below some sequence's new tokens, whose rows past it are left as they are."""
+    import torch
+    banner(f"attn4 many prompts D={D} G={G}")
+    H = 64 if G == 3 else 32
+    new = [30, 25, 30, 1, 30, 0, 28, 30, 12, 30] if G == 3 else [30, 7, 25, 0, 30]
+    lens = [30, 200, 64, 1, 25, 0, 129, 31, 90, 65] if G == 3 else [40, 100, 20, 0, 130]
+    c = Case4(31, lens, new, H * G, H, D, 64)
+    out = c.run()
+    c.check(out)
+    again = c.run(max_len=2000)
+    torch.cuda.synchronize()
+    assert torch.equal(again.view(torch.int16), out.view(torch.int16))
+    res = torch.full_like(out, 7.0)
+    bound = 26
+    tl.attention(c.q_dev(), c.cache.device(), _int(c.table), _int(c.lens), _int(c.offsets), bound, max(lens), c.scale, out=res)
+    torch.cuda.synchronize()
+    for b, n in enumerate(new):
+        a = int(c.offsets[b])
+        assert torch.equal(res[a:a + min(n, bound)].view(torch.int16), out[a:a + min(n, bound)].view(torch.int16))
+        assert (res[a + min(n, bound):a + n] == 7.0).all()
