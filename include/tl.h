@@ -686,8 +686,8 @@ typedef struct tl_kv_pages {
  * and 'missing' counts it twice.
  * Errors: TL_EINVAL for NULL or misaligned pointers (4 bytes), sizes below 1, a
  * bad page_tokens, more than 2^31 - 1 tokens, n < 0, or arrays that overlap;
- * TL_EUNSUPPORTED for max_pages of 2^31 or more or n above 65536; TL_ENOMEM if
- * the workspace cannot be allocated.
+ * TL_EUNSUPPORTED for max_pages above 2^25, num_rows * max_pages above 2^40 or n
+ * above 65536; TL_ENOMEM if the workspace cannot be allocated.
  */
 int tl_kv_grow(const tl_kv_pages* pages, const int32_t* rows, const int32_t* lens, int32_t n, int32_t* missing, void* stream);
 

@@ -53,23 +53,6 @@ __device__ inline int64_t uniform(int64_t x) {
     return int64_t(uint64_t(uint32_t(uniform(int(x >> 32)))) << 32 | uint32_t(uniform(int(x))));
 }
 
-// a / b of a >= 0, b > 0 below 2^53.  A workgroup makes six such divisions in a row
-// before its first load.  Below 2^31: by way of a float's reciprocal, off by at
-// most 2^-21 of itself, and of that of what is left (below 2^10 b, so that the
-// second is off by less than one): 20 instructions; else by way of a double, 50,
-// and a sixth of a 64-bit integer division's.
-__device__ inline int64_t quotient(int64_t a, int64_t b) {
-    if (uint64_t(a) < 0x80000000u && uint64_t(b) < 0x80000000u) {
-        const float inv = __builtin_amdgcn_rcpf(float(int(b)));
-        int q = int(float(int(a)) * inv);
-        q += int(float(int(uint32_t(a) - uint32_t(q) * uint32_t(b))) * inv);
-        const int r = int(uint32_t(a) - uint32_t(q) * uint32_t(b));
-        return q + (r >= int(b)) - (r < 0);
-    }
-    const int64_t q = int64_t(double(a) / double(b)), r = a - q * b;
-    return q + (r >= b) - (r < 0);
-}
-
 // Memory that no kernel writes while this one runs: uniform reads of it are
 // scalar loads, which vector loads in flight do not hold up.
 typedef const __attribute__((address_space(4))) int32_t* ConstInts;

@@ -163,17 +163,18 @@ __device__ void grow_give(const PagesLaunch& a, const Crew& w, int32_t* pages) {
     for (int64_t i = w.wave; i < max(a.n, int64_t(1)); i += w.waves) {
         const int want = a.n ? a.want[i] : 0;
         if (want == 0 && i < a.n - 1) continue;
+        // the first entries are on their way while the sums are made
+        int32_t* row = want ? row_of(a, a.rows[i]) : nullptr;
+        const int need = want ? pages_of(a, a.lens[i]) : 0, first = want ? a.first[i] : 0;
+        int old = first + w.lane < need ? row[first + w.lane] : 0;
         int64_t rank = sum_of(a.want, i, w.lane);
         if (i >= a.n - 1) {                                 // the last one knows them all
             const int64_t missing = rank + want - sum_of(a.free, a.blocks, w.lane);
             if (w.lane == 0) *a.count = int32_t(max(int64_t(0), missing));
         }
-        if (want == 0) continue;
-        int32_t* row = row_of(a, a.rows[i]);
-        const int need = pages_of(a, a.lens[i]);
         PageCursor c{0, 0};
-        for (int base = a.first[i]; base < need; base += 64) {
-            const int old = base + w.lane < need ? row[base + w.lane] : 0;
+        for (int base = first; base < need; base += 64) {
+            if (base > first) old = base + w.lane < need ? row[base + w.lane] : 0;
             const u64 none = __ballot(old < 0);
             if (!none) continue;
             const int got = page_take(a, w, rank, __popcll(none), &c, pages);
@@ -355,13 +356,15 @@ template <int BYTES, int EXPS>      // of a token's head: of keys (and of values
 __global__ __launch_bounds__(kThreads) void pages_copy_kernel(PagesCopyLaunch a) {
     constexpr int kChunks = 64 * BYTES / 16, kLoads = (kChunks + kThreads - 1) / kThreads;
     const int log2_groups = a.c.log2_page - 6, per = a.c.heads << log2_groups;
-    const int64_t pairs = a.count ? min(max(int64_t(*a.count), int64_t(0)), a.pairs) : a.pairs;
-    for (int64_t u = blockIdx.x; u < pairs * per; u += gridDim.x) {
-        const int64_t pair = u / per;
+    const int64_t count = a.count ? *a.count : a.pairs;
+    for (int64_t u = blockIdx.x; u < a.pairs * per; u += gridDim.x) {
+        const int64_t pair = quotient(u, per);
         const int rest = int(u - pair * per), group = rest & ((1 << log2_groups) - 1);
+        // the pair is loaded while it is not known yet whether it is one
         const int64_t src = a.src[pair], dst = a.dst[pair];
-        if (src < 0 || src >= a.c.num_pages || dst < 0 || dst >= a.c.num_pages || src == dst) continue;
-        if (a.tokens && group * 64 >= a.tokens[pair]) continue;
+        const int tokens = a.tokens ? a.tokens[pair] : 1 << a.c.log2_page;
+        if (pair >= count) break;
+        if (src < 0 || src >= a.c.num_pages || dst < 0 || dst >= a.c.num_pages || src == dst || group * 64 >= tokens) continue;
         const int64_t from = (src * per + rest) * 64, to = (dst * per + rest) * 64;        // tokens of one head
         const u32x4 *k0 = reinterpret_cast<const u32x4*>(a.c.k + from * BYTES), *v0 = reinterpret_cast<const u32x4*>(a.c.v + from * BYTES);
         u32x4 *k1 = reinterpret_cast<u32x4*>(a.c.k + to * BYTES), *v1 = reinterpret_cast<u32x4*>(a.c.v + to * BYTES);

@@ -67,7 +67,7 @@ int check_pages(const tl_kv_pages* p, int64_t n, std::initializer_list<const int
     if (bad_pointer(p->refs, 4) || bad_pointer(p->page_table, 4)) return TL_EINVAL;
     for (const int32_t* list : lists)
         if (n > 0 && bad_pointer(list, 4)) return TL_EINVAL;
-    if (p->max_pages > kMaxInt || n > kMostPageRows) return TL_EUNSUPPORTED;
+    if (p->max_pages > kMostRowPages || p->num_rows > kMostEntries / p->max_pages || n > kMostPageRows) return TL_EUNSUPPORTED;
     if (overlap({p->refs, p->num_pages * 4}, {p->page_table, p->max_pages * p->num_rows * 4})) return TL_EINVAL;
     a->refs = p->refs;
     a->table = p->page_table;

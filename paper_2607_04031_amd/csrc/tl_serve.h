@@ -123,6 +123,7 @@ constexpr int kPagesGrow = 0, kPagesFork = 1, kPagesCompact = 2;
 constexpr int kPageThreads = 256;
 constexpr int kPageBlock = 4096;    // pages whose bits a wave makes
 constexpr int kMostPageRows = 65536;
+constexpr int64_t kMostRowPages = int64_t(1) << 25, kMostEntries = int64_t(1) << 40;    // of a row, and of a table
 struct PagesLaunch {
     int32_t* refs;
     int32_t* table;             // [num_rows][max_pages]

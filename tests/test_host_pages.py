@@ -42,6 +42,7 @@ BAD_POOLS = [(dict(refs=None), tl.TL_EINVAL), (dict(refs=addr(0) + 2), tl.TL_EIN
              (dict(page_table=addr(1) + 1), tl.TL_EINVAL), (dict(num_pages=0), tl.TL_EINVAL), (dict(max_pages=0), tl.TL_EINVAL),
              (dict(num_rows=0), tl.TL_EINVAL), (dict(page_tokens=32), tl.TL_EINVAL), (dict(page_tokens=96), tl.TL_EINVAL),
              (dict(page_tokens=8192), tl.TL_EINVAL), (dict(num_pages=1 << 25), tl.TL_EINVAL), (dict(max_pages=1 << 31), tl.TL_EUNSUPPORTED),
+             (dict(max_pages=(1 << 25) + 1), tl.TL_EUNSUPPORTED), (dict(max_pages=1 << 25, num_rows=(1 << 15) + 1), tl.TL_EUNSUPPORTED),
              (dict(page_table=addr(0) + 3996), tl.TL_EINVAL), (dict(refs=addr(1) + 8 * 30 * 4 - 4), tl.TL_EINVAL)]
 
 
