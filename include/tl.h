@@ -681,7 +681,7 @@ typedef struct tl_kv_pages {
  *
  * rows, lens: device int32 [n].
  * missing:    device int32 [1]: how many entries found no free page (they, and
- *             only they, stay negative).  Always written.
+ *             only they, stay negative), at most 2^31 - 1.  Always written.
  * A row that is named twice gets its pages once, which ones is not specified,
  * and 'missing' counts it twice.
  * Errors: TL_EINVAL for NULL or misaligned pointers (4 bytes), sizes below 1, a
@@ -705,7 +705,8 @@ int tl_kv_free(const tl_kv_pages* pages, const int32_t* rows, const int32_t* len
  * pages are shared (a reference more); a page that they fill in part is the
  * child's own, a free one, and a pair of pages to copy (tl_kv_copy, once for
  * every cache of the pool).  What the child's row held before loses its
- * references; its other entries become -1.
+ * references; its other entries become -1.  A parent outside the table has no
+ * tokens.
  *
  * parents, children, lens: device int32 [n]; lens are clamped to the table's
  *             width.

@@ -170,7 +170,7 @@ __device__ void grow_give(const PagesLaunch& a, const Crew& w, int32_t* pages) {
         int64_t rank = sum_of(a.want, i, w.lane);
         if (i >= a.n - 1) {                                 // the last one knows them all
             const int64_t missing = rank + want - sum_of(a.free, a.blocks, w.lane);
-            if (w.lane == 0) *a.count = int32_t(max(int64_t(0), missing));
+            if (w.lane == 0) *a.count = int32_t(min(max(int64_t(0), missing), int64_t(INT32_MAX)));
         }
         PageCursor c{0, 0};
         for (int base = first; base < need; base += 64) {

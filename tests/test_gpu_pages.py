@@ -50,6 +50,16 @@ def test_grow(pages, rows, width, load):
     assert pool.counts_hold()
 
 
+def test_grow_missing_past_31_bits():
+    import torch
+    banner("pages grow: a row of 2^25 entries, named 66 times, one page")
+    width = 2 ** 25                                        # 66 * 2^25 - 1 entries go without: more than int32 holds
+    dev = tl.kv_pages(1, 1, width)
+    missing = tl.kv_grow(dev, torch.zeros(66, dtype=torch.int32, device="cuda"), torch.full((66,), 2 ** 31 - 1, dtype=torch.int32, device="cuda"))
+    assert missing.tolist() == [2 ** 31 - 1] and dev.refs.tolist() == [1]
+    assert int(dev.table[0, 0]) == 0 and int((dev.table == -1).sum()) == width - 1
+
+
 @pytest.mark.parametrize("pages,rows,width", SIZES)
 def test_free(pages, rows, width):
     banner(f"pages free: {pages} pages, {rows} x {width}")
