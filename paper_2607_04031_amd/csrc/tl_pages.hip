@@ -24,8 +24,8 @@ namespace tl {
 namespace {
 
 constexpr int kThreads = kPageThreads;
-constexpr int kWide = 1024;             // threads of a call that is one workgroup, for so many blocks and sequences
-constexpr int kFewBlocks = 16, kFewRows = 64;
+constexpr int kWide = 1024;             // threads of a call that is one workgroup: a wave for each of so many sequences
+constexpr int kFewBlocks = 4, kFewRows = 16, kFewEntries = 64;     // blocks of pages; the table's entries, in waves' loads
 constexpr int kBlock = kPageBlock;      // pages of a wave's bits: a word of 64 a lane
 typedef unsigned long long u64;
 
@@ -394,8 +394,12 @@ uint32_t groups_of(int64_t waves) { return uint32_t(std::max<int64_t>(1, (waves 
 template <int OP>
 hipError_t launch_phases(const PagesLaunch& given, int64_t first, int64_t second, int64_t third, hipStream_t stream) {
     PagesLaunch a = given;
-    // one workgroup of sixteen waves where none has more than a few things to do
-    if (a.blocks <= kFewBlocks && second <= kFewRows && third <= 64) {
+    // One workgroup of sixteen waves where each has a block, a sequence and a few entries at most.  As one workgroup and as
+    // launches, us: grow of 1000 pages, 16 rows 4.3 and 5.0, 64 rows 6.4 and 5.3; of 16000, 6.6 and 7.1, 8.6 and 7.5; of
+    // 60000, 16 rows, 11.4 and 7.3.  fork of 1000 pages, 4 rows 7.6 and 8.6, 64 rows 34 and 11.8; of 16000, 16 rows 12.7 and
+    // 12.5; of 60000 17.3 and 12.5.  compact of 1000 pages, 4096 entries 11.2 and 13.9, 8192 entries 12.4 and 14.0, 16384 15.3
+    // and 14.0; of 16000 pages 18.4 and 18.7, 22.2 and 18.4, 24.7 and 18.6; of 60000, 512 entries, 30 and 17.
+    if (a.blocks <= kFewBlocks && second <= kFewRows && third <= kFewEntries) {
         hipLaunchKernelGGL((pages_kernel<OP, 0>), dim3(1), dim3(kWide), 0, stream, a);
         return hipGetLastError();
     }
