@@ -2,110 +2,20 @@
 // plan, dispatch.  Nothing is enqueued unless every check passes.
 #include <algorithm>
 #include <cmath>
-#include <initializer_list>
 
 #include "tl_internal.h"
 #include "tl_serve.h"
+#include "tl_serve_check.h"
 
 namespace tl {
 namespace {
 
-constexpr int64_t kMaxInt = 0x7fffffff;
 constexpr int64_t kMaxStride = int64_t(1) << 30;
 constexpr int kMaxNodes = 4096;
 constexpr float kLog2e = 1.44269504088896340736f;
 
-bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
-bool bad_pointer(const void* p, uintptr_t to) { return !p || !aligned(p, to); }
-
-struct Range {
-    const void* p;
-    int64_t bytes;
-};
-bool overlap(const Range& a, const Range& b) {
-    if (!a.p || !b.p || a.bytes <= 0 || b.bytes <= 0) return false;
-    const auto x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
-    return x < y + uintptr_t(b.bytes) && y < x + uintptr_t(a.bytes);
-}
-
-// The cache's sizes; data and exps: bytes of k (v) and of k_exp (v_exp).
-int check_sizes(const tl_kv_cache* c, int64_t* data, int64_t* exps) {
-    if (!c || c->num_pages < 1 || !is_pow2(c->page_tokens) || c->page_tokens < 64 || c->page_tokens > 4096) return TL_EINVAL;
-    if (c->kv_heads < 1 || c->kv_heads > 1024 || (c->elem_bytes != 1 && c->elem_bytes != 2 && c->elem_bytes != TL_KV_E2M1)) return TL_EINVAL;
-    if (c->num_pages > kMaxInt / c->page_tokens) return TL_EINVAL;
-    if (c->head_dim != 64 && c->head_dim != 128) return TL_EUNSUPPORTED;
-    const int64_t tokens = c->num_pages * c->page_tokens * c->kv_heads;
-    const bool four = c->elem_bytes == TL_KV_E2M1;
-    *data = four ? tokens * c->head_dim / 2 : tokens * c->head_dim * c->elem_bytes;
-    *exps = four ? tokens * c->head_dim / 32 : c->elem_bytes == 1 ? tokens : 0;
-    return TL_OK;
-}
-
-int check_cache(const tl_kv_cache* c, int64_t* data, int64_t* exps, KvView* view) {
-    const int rc = check_sizes(c, data, exps);
-    if (rc != TL_OK) return rc;
-    if (bad_pointer(c->k, 16) || bad_pointer(c->v, 16)) return TL_EINVAL;
-    if (*exps && (bad_pointer(c->k_exp, 16) || bad_pointer(c->v_exp, 16))) return TL_EINVAL;
-    *view = KvView{static_cast<uint8_t*>(c->k), static_cast<uint8_t*>(c->v), c->k_exp, c->v_exp, c->num_pages,
-                   ilog2(c->page_tokens), c->kv_heads};
-    return TL_OK;
-}
-
-bool hits_cache(const tl_kv_cache* c, int64_t data, int64_t exps, const Range& r) {
-    return overlap(r, {c->k, data}) || overlap(r, {c->v, data}) || overlap(r, {c->k_exp, exps}) || overlap(r, {c->v_exp, exps});
-}
-
-int done(hipError_t e) { return e == hipSuccess ? TL_OK : TL_EHIP; }
-
 // Bytes from the first row's start to the last row's end.
 int64_t span(int64_t rows, int64_t ld, int64_t width, int64_t elem) { return rows > 0 ? ((rows - 1) * ld + width) * elem : 0; }
-
-// A pool's sizes and pointers, and lists of n entries each (not looked at where n is 0).
-int check_pages(const tl_kv_pages* p, int64_t n, std::initializer_list<const int32_t*> lists, PagesLaunch* a) {
-    if (!p || p->num_pages < 1 || p->num_rows < 1 || p->max_pages < 1 || n < 0) return TL_EINVAL;
-    if (!is_pow2(p->page_tokens) || p->page_tokens < 64 || p->page_tokens > 4096 || p->num_pages > kMaxInt / p->page_tokens) return TL_EINVAL;
-    if (bad_pointer(p->refs, 4) || bad_pointer(p->page_table, 4)) return TL_EINVAL;
-    for (const int32_t* list : lists)
-        if (n > 0 && bad_pointer(list, 4)) return TL_EINVAL;
-    if (p->max_pages > kMostRowPages || p->num_rows > kMostEntries / p->max_pages || n > kMostPageRows) return TL_EUNSUPPORTED;
-    if (overlap({p->refs, p->num_pages * 4}, {p->page_table, p->max_pages * p->num_rows * 4})) return TL_EINVAL;
-    a->refs = p->refs;
-    a->table = p->page_table;
-    a->num_pages = p->num_pages;
-    a->max_pages = p->max_pages;
-    a->num_rows = p->num_rows;
-    a->log2_page = ilog2(p->page_tokens);
-    a->n = n;
-    a->blocks = (p->num_pages + kPageBlock - 1) / kPageBlock;
-    return TL_OK;
-}
-
-// whether outputs overlap the pool, lists of n entries or one another, or lists the pool
-bool hits(const tl_kv_pages* p, int64_t n, std::initializer_list<const int32_t*> lists, std::initializer_list<Range> outs) {
-    const Range refs = {p->refs, p->num_pages * 4}, table = {p->page_table, p->max_pages * p->num_rows * 4};
-    for (const Range* r = outs.begin(); r != outs.end(); ++r) {
-        if (overlap(*r, refs) || overlap(*r, table)) return true;
-        for (const int32_t* list : lists)
-            if (overlap(*r, {list, n * 4})) return true;
-        for (const Range* other = outs.begin(); other != r; ++other)
-            if (overlap(*r, *other)) return true;
-    }
-    for (const int32_t* list : lists)
-        if (overlap({list, n * 4}, refs) || overlap({list, n * 4}, table)) return true;
-    return false;
-}
-
-int pages_workspace(PagesLaunch* a, int64_t n, StreamHold* hold, void* stream) {
-    void* ws = nullptr;
-    const int st = stream_workspace((hipStream_t)stream, size_t(a->blocks * (64 * 12 + 4) + n * 8), hold, &ws);
-    if (st != TL_OK) return st;
-    a->map = static_cast<unsigned long long*>(ws);
-    a->before = reinterpret_cast<int32_t*>(a->map + a->blocks * 64);
-    a->free = a->before + a->blocks * 64;
-    a->want = a->free + a->blocks;
-    a->first = a->want + n;
-    return TL_OK;
-}
 
 }  // namespace
 
@@ -263,90 +173,6 @@ int tl_kv_keep(const tl_kv_cache* cache, const int32_t* page_table, int64_t max_
     a.num_seqs = num_seqs;
     a.max_path = int(max_path);
     return done(launch_kv_keep(a, cache->head_dim, cache->elem_bytes, (hipStream_t)stream));
-}
-
-int tl_kv_grow(const tl_kv_pages* pages, const int32_t* rows, const int32_t* lens, int32_t n, int32_t* missing, void* stream) {
-    PagesLaunch a{};
-    const int rc = check_pages(pages, n, {rows, lens}, &a);
-    if (rc != TL_OK) return rc;
-    if (bad_pointer(missing, 4) || hits(pages, n, {rows, lens}, {{missing, 4}})) return TL_EINVAL;
-    a.rows = rows;
-    a.lens = lens;
-    a.count = missing;
-    StreamHold hold;
-    const int st = pages_workspace(&a, n, &hold, stream);
-    return st != TL_OK ? st : done(launch_pages_grow(a, (hipStream_t)stream));
-}
-
-int tl_kv_free(const tl_kv_pages* pages, const int32_t* rows, const int32_t* lens, int32_t n, void* stream) {
-    PagesLaunch a{};
-    const int rc = check_pages(pages, n, {rows, lens ? lens : rows}, &a);
-    if (rc != TL_OK) return rc;
-    if (hits(pages, n, {rows, lens}, {})) return TL_EINVAL;
-    a.rows = rows;
-    a.lens = lens;
-    return n == 0 ? TL_OK : done(launch_pages_free(a, (hipStream_t)stream));
-}
-
-int tl_kv_fork(const tl_kv_pages* pages, const int32_t* parents, const int32_t* children, const int32_t* lens, int32_t n,
-               int32_t* src, int32_t* dst, int32_t* tokens, int32_t* count, void* stream) {
-    PagesLaunch a{};
-    const int rc = check_pages(pages, n, {parents, children, lens}, &a);
-    if (rc != TL_OK) return rc;
-    if (bad_pointer(count, 4) || (n > 0 && (bad_pointer(src, 4) || bad_pointer(dst, 4) || bad_pointer(tokens, 4)))) return TL_EINVAL;
-    const int64_t list = int64_t(n) * 4;
-    if (hits(pages, n, {parents, children, lens}, {{src, list}, {dst, list}, {tokens, list}, {count, 8}})) return TL_EINVAL;
-    a.parents = parents;
-    a.rows = children;
-    a.lens = lens;
-    a.src = src;
-    a.dst = dst;
-    a.tokens = tokens;
-    a.count = count;
-    StreamHold hold;
-    const int st = pages_workspace(&a, n, &hold, stream);
-    return st != TL_OK ? st : done(launch_pages_fork(a, (hipStream_t)stream));
-}
-
-int tl_kv_compact(const tl_kv_pages* pages, int64_t max_moves, int32_t* src, int32_t* dst, int32_t* count, void* stream) {
-    PagesLaunch a{};
-    const int rc = check_pages(pages, 0, {}, &a);
-    if (rc != TL_OK) return rc;
-    if (max_moves < 0 || bad_pointer(count, 4) || (max_moves > 0 && (bad_pointer(src, 4) || bad_pointer(dst, 4)))) return TL_EINVAL;
-    if (max_moves > kMaxInt) return TL_EUNSUPPORTED;
-    if (hits(pages, 0, {}, {{src, max_moves * 4}, {dst, max_moves * 4}, {count, 8}})) return TL_EINVAL;
-    a.n = max_moves;
-    a.src = src;
-    a.dst = dst;
-    a.count = count;
-    StreamHold hold;
-    const int st = pages_workspace(&a, 0, &hold, stream);
-    return st != TL_OK ? st : done(launch_pages_compact(a, (hipStream_t)stream));
-}
-
-int tl_kv_copy(const tl_kv_cache* cache, const int32_t* src, const int32_t* dst, const int32_t* tokens, const int32_t* count,
-               int64_t max_pairs, void* stream) {
-    int64_t data, exps;
-    PagesCopyLaunch a{};
-    const int rc = check_cache(cache, &data, &exps, &a.c);
-    if (rc != TL_OK) return rc;
-    if (max_pairs < 0 || !aligned(tokens, 4) || !aligned(count, 4)) return TL_EINVAL;
-    if (max_pairs == 0) return TL_OK;
-    if (bad_pointer(src, 4) || bad_pointer(dst, 4)) return TL_EINVAL;
-    if (max_pairs > kMaxInt) return TL_EUNSUPPORTED;
-    const Range lists[4] = {{src, max_pairs * 4}, {dst, max_pairs * 4}, {tokens, max_pairs * 4}, {count, 4}};
-    for (const Range& r : lists)
-        if (hits_cache(cache, data, exps, r)) return TL_EINVAL;
-    const Range arrays[4] = {{cache->k, data}, {cache->v, data}, {cache->k_exp, exps}, {cache->v_exp, exps}};
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < i; ++j)
-            if (overlap(arrays[i], arrays[j])) return TL_EINVAL;
-    a.src = src;
-    a.dst = dst;
-    a.tokens = tokens;
-    a.count = count;
-    a.pairs = max_pairs;
-    return done(launch_pages_copy(a, cache->head_dim, cache->elem_bytes, (hipStream_t)stream));
 }
 
 int tl_attn(const void* Q, int64_t ldq, const tl_kv_cache* cache, const int32_t* page_table, int64_t max_pages,

@@ -1,6 +1,6 @@
 // Internal declarations of the serving-step operators: the paged key/value
 // cache (tl_kv.hip), its pages (tl_pages.hip), attention over it (tl_attn.hip)
-// and the verification of drafted tokens (tl_verify.hip).  The entry points in tl_serve.cpp check all
+// and the verification of drafted tokens (tl_verify.hip).  The entry points in tl_serve.cpp and tl_pages.cpp check all
 // arguments; the launchers only enqueue.
 #pragma once
 
