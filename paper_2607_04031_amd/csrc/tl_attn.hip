@@ -17,10 +17,20 @@
 // The sum l is of the unrounded ones.  Against 64 bits the error is 2.2e-3 of
 // the result, of which the output's own rounding is 1.7e-3.
 //
+// 4-bit entries become bf16 with their scales, keys and values (exact: two
+// significant bits times a power of two), as fast as an fma per pair; a byte of
+// the values holds elements d and d + 16, so that two of a lane's pairs, sorted by
+// v_perm, are the operands of two blocks of the head.  Any code is finite, so that
+// infinities and NaNs are looked for among the scales, 64 tokens at a time, and
+// among the values only where a scale can make them.  The scaled MFMA, which
+// takes E2M1 as it lies, is not used: its sum was off by 8.5e-5 of sum |ab|.
+//
 // Single tokens are bound by HBM: 32 sequences of up to 8192 tokens, 64 heads
-// over 8, 8 bits: 59 us, 5.7 TB/s, and 4.8 us for the join.  Few chunks per
+// over 8, 8 bits: 59 us, 5.7 TB/s, and 4.8 us for the join; 4 bits: 36 us, 4.9
+// TB/s (6.3 in the middle; a workgroup's start takes over 3 us), and 4.7.  Few chunks per
 // workgroup are bound by its start and end: three chains of five tokens over
-// 131072, 8 heads over one, 30 us (2.5 TB/s) and 7 us; one token over 517, 7 us.
+// 131072, 8 heads over one, 30 us (2.5 TB/s) and 7 us, 4 bits 25 (conversions, made
+// by both waves that share the keys) and 7.6; one token over 517, 7 us, 4 bits 7.6.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -64,7 +74,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     if (threadIdx.x == 0) odd_any = 0;
     __syncthreads();
     while (run.place < run.end) {
-        const AttnPiece piece = attn_piece<D>(a, &line, &run);
+        const AttnPiece piece = attn_piece<D, false>(a, &line, &run);
         const Seq& s = piece.s;
         const int head = piece.head, tile = piece.tile;
         // keys below 'all' are seen by every row of the wave, keys from 'end' on by none

@@ -53,6 +53,14 @@ __device__ inline int64_t uniform(int64_t x) {
     return int64_t(uint64_t(uint32_t(uniform(int(x >> 32)))) << 32 | uint32_t(uniform(int(x))));
 }
 
+// x, as a value that the compiler does not see through: what is computed of it is not computed ahead of loops, where
+// it would hold registers
+template <typename T>
+__device__ inline T hidden(T x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 // Memory that no kernel writes while this one runs: uniform reads of it are
 // scalar loads, which vector loads in flight do not hold up.
 typedef const __attribute__((address_space(4))) int32_t* ConstInts;
@@ -119,7 +127,7 @@ __device__ inline int64_t attn_total(const AttnLaunch& a, AttnLine* line) {
 
 // The sequence that holds place p (below the total).
 __device__ inline Seq attn_find(const AttnLaunch& a, const AttnLine* line, int64_t p) {
-    const int lane = threadIdx.x & 63;
+    const int lane = hidden(int(threadIdx.x & 63));
     Seq s{};
     int64_t before = 0;
     if (a.num_seqs <= 64) {
@@ -229,7 +237,7 @@ struct AttnPiece {
 // more than k chunks are its last ones, of a number in closed form; k is found by
 // bisection of the sum over sequences.
 __device__ inline void attn_sorted(const AttnLaunch& a, const AttnLine* line, int64_t p, AttnPiece* piece) {
-    const int lane = threadIdx.x & 63;
+    const int lane = hidden(int(threadIdx.x & 63)), heads = uniform(hidden(a.c.heads));
     Seq s{};
     if (lane < a.num_seqs) {
         s.n = line->n[lane];
@@ -244,7 +252,7 @@ __device__ inline void attn_sorted(const AttnLaunch& a, const AttnLine* line, in
         if (a.mask || keys <= start) return s.tiles;
         return s.tiles - (int(((keys - start) * a.group + rows) >> a.log2_rows) - 1);      // the first whose last row's token is keys - start or later
     };
-    auto all_longer = [&](int k) { return over_lanes(int64_t(longer(k))) * a.c.heads; };
+    auto all_longer = [&](int k) { return over_lanes(int64_t(longer(k))) * heads; };
     int most = s.tiles ? (s.len + (1 << a.log2_keys) - 1) >> a.log2_keys : 0;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) most = max(most, __shfl_xor(most, d));
@@ -256,7 +264,7 @@ __device__ inline void attn_sorted(const AttnLaunch& a, const AttnLine* line, in
     }
     // of those of lo chunks the item-th
     const int64_t left = p - all_longer(lo);
-    const int item = uniform(int(quotient(left, a.c.heads)));
+    const int item = uniform(int(quotient(left, heads)));
     const int after = longer(lo), mine = (lo ? longer(lo - 1) : s.tiles) - after, upto = upto_lane(mine);
     const int who = uniform(__builtin_ctzll(__ballot(upto > item) | 1ull << 63));
     piece->s.seq = who;
@@ -264,20 +272,21 @@ __device__ inline void attn_sorted(const AttnLaunch& a, const AttnLine* line, in
     piece->s.n = uniform(line->n[who]);
     piece->s.len = uniform(line->len[who]);
     attn_sizes(a, &piece->s);
-    piece->head = uniform(int(left - int64_t(item) * a.c.heads));
+    piece->head = uniform(int(left - int64_t(item) * heads));
     piece->tile = piece->s.tiles - 1 - of_lane(after, who) - (item - of_lane(upto - mine, who));
 }
-template <int D>
+template <int D, bool MAY_SORT>
 __device__ inline AttnPiece attn_piece(const AttnLaunch& a, const AttnLine* line, AttnRun* r) {
     AttnPiece p;
-    if (a.sorted) attn_sorted(a, line, r->place, &p);
+    const bool sorted = MAY_SORT && a.sorted;
+    if (sorted) attn_sorted(a, line, r->place, &p);
     else p.s = attn_find(a, line, r->place);
     const int64_t in_seq = r->place - p.s.before;
     if (a.split) {
         const int64_t per_head = attn_cost(p.s, p.s.tiles);
         p.head = uniform(int(quotient(in_seq, per_head)));
         p.tile = uniform(attn_tile_at(p.s, in_seq - p.head * per_head));
-    } else if (!a.sorted) {
+    } else if (!sorted) {
         p.head = uniform(int(quotient(in_seq, p.s.tiles)));
         p.tile = p.s.tiles - 1 - uniform(int(in_seq - int64_t(p.head) * p.s.tiles));    // the longest first
     }
@@ -301,7 +310,7 @@ __device__ inline AttnPiece attn_piece(const AttnLaunch& a, const AttnLine* line
     p.slot = 2 * int64_t(r->me) + (start > r->place0 ? 1 : 0);
     r->place = start + to;
     if (start >= r->place0 && to < places && threadIdx.x == 0)      // others go on with it
-        attn_shared<D>(a)[r->me] = AttnShared{p.s.first, p.s.rows, p.head, p.tile, attn_group_of(start + places - 1, r->total, r->groups), int(p.slot)};
+        attn_shared<D>(a)[r->me] = AttnShared{p.s.first, p.s.rows, p.head, p.tile, attn_group_of(start + places - 1, hidden(r->total), r->groups), int(p.slot)};
     return p;
 }
 

@@ -1,7 +1,7 @@
 // Attention for many rows per sequence and key head (prompts, large trees): the
 // products of attn_kernel (tl_attn.hip) for 128 rows, 32 a wave, whose four
 // waves share every chunk of 64 keys.  A chunk is loaded once per workgroup, as
-// it lies in the pages, a chunk ahead; on its way into LDS 8-bit entries become
+// it lies in the pages, a chunk ahead; on its way into LDS 4- and 8-bit entries become
 // bf16 operands, once instead of once per wave.  Two chunks' buffers: one is
 // filled while the other is read, one barrier a chunk.  Operands of one
 // instruction are 1 KB without gaps in LDS, so reads have no bank conflicts.
@@ -10,7 +10,13 @@
 // only in part (MFMA busy for 36 % of the cycles, 8 bits 32 %, at 2.12 - 2.15
 // GHz), and by the starts and ends of pieces of tiles.  Three prompts, 135
 // GFLOP, bf16: 153 - 155 us, the join of partial results 13.5; trees of 64
-// tokens, 107 GFLOP over 8-bit entries, 151 - 160 us, the join 10.3.
+// tokens, 107 GFLOP over 8-bit entries, 151 - 160 us, the join 10.3.  Prompts over
+// 4-bit entries, 135 GFLOP, 146 - 154 us without a join (whole tiles, the longest
+// first), 172 and 13.4 in equal parts: of a chunk's 3.7 thousand cycles a wave
+// converts for 674, loads for 378, multiplies for 937 and 1131, takes 405 for the softmax
+// and 199 at the barrier.  4 bits sum the weights, rounded as the products take
+// them, by a product with ones (2 of 34 MFMA, for 32 additions a lane), and have
+// both row tiles' softmax run side by side.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -40,13 +46,6 @@ __device__ inline void load_to_lds(const uint8_t* base, uint32_t voff, u32x4* ld
 #pragma clang diagnostic pop
 }
 
-// x, as a value that the compiler does not see through: what is computed of it is not computed ahead of loops, where
-// it would hold registers
-__device__ inline int hidden(int x) {
-    asm volatile("" : "+v"(x));
-    return x;
-}
-
 template <int D, int ELEM>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) void attn_wide_kernel(AttnLaunch a) {
     constexpr int kSteps = D / 32;                 // MFMA steps along the head
@@ -68,9 +67,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     if (threadIdx.x == 0) odd_any = 0;
     __syncthreads();
     while (run.place < run.end) {
-        const AttnPiece piece = attn_piece<D>(a, &line, &run);
+        const AttnPiece piece = attn_piece<D, kFour>(a, &line, &run);
         const Seq& s = piece.s;
-        const int thread = hidden(threadIdx.x), lane = thread & 63, g = lane >> 4, col = lane & 15;
+        const int thread = hidden(int(threadIdx.x)), lane = thread & 63, g = lane >> 4, col = lane & 15;
         // keys below 'all' are seen by every row, keys from 'end' on by none: of the workgroup's, and of the wave's
         const int start = s.len - s.n;
         auto all_of = [&](int first) { return max(0, min(s.len, a.mask ? start : start + attn_token(a, first) + 1)); };
@@ -426,7 +425,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
                 for (int nt = 0; nt < kRowTiles; ++nt) attn_odd_chunk<D, ELEM, 4>(a, piece, c, at, row0 + nt * 16 + col, odd_s);
             }
         }
-        const int lane2 = hidden(threadIdx.x & 63), g2 = lane2 >> 4, col2 = lane2 & 15;
+        const int lane2 = hidden(int(threadIdx.x & 63)), g2 = lane2 >> 4, col2 = lane2 & 15;
         // a wave's results, a row tile at a time, through LDS of its own
         float* mine = reinterpret_cast<float*>(kv_s) + wave * 16 * kPad;
 #pragma unroll
