@@ -42,7 +42,9 @@ __device__ inline int64_t exps_at(const KvView& c, int64_t page, int head) { ret
 // launch bounds it.  Many tokens (windows): queries a token per workgroup, keys
 // 16 tokens and values 64 tokens of a head, so that whole cache lines are
 // written where the slots follow one another; HBM bounds it (8192 rows of 64
-// heads over 8: 70 us, 4.8 TB/s; a single row: 3.5 us).
+// heads over 8: 70 us, 4.8 TB/s, in 4 bits 70 - 75 us, of whose bytes 86 % are the
+// queries'; a single row: 3.5 us, in 4 bits 3.4).  4-bit values: a lane and the
+// one two on swap codes, so that each has whole bytes (elements d and d + 16).
 // ---------------------------------------------------------------------------
 constexpr int kKeyWindow = 16, kValueWindow = 64;
 
@@ -628,7 +630,8 @@ __global__ __launch_bounds__(kThreads) void kv_keep_kernel(KvKeepLaunch a) {
 }
 
 // Rows from which windows are taken: us at 64 heads over 8, per token and in windows, 256 rows 6.0 and 7.3 (append),
-// 512 10.4 and 8.5, 8192 119 and 72; read, 512 3.4 and 4.0, 1024 4.5 and 4.2, 8192 22.8 and 10.7.
+// 512 10.4 and 8.5, 8192 119 and 72; read, 512 3.4 and 4.0, 1024 4.5 and 4.2, 8192 22.8 and 10.7.  4 bits: append, 256
+// rows 5.2 and 6.0, 512 8.1 and 8.2, 2048 21.8 and 18.0; read, 512 4.1 and 4.1, 1024 4.7 and 4.3, 4096 12.4 and 6.7.
 constexpr int64_t kAppendWindowRows = 512, kReadWindowRows = 1024;
 
 // All workgroups; *b: in windows.

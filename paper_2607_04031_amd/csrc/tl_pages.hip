@@ -12,7 +12,14 @@
 //
 // A call is a chain of phases, each of which needs the one before whole: as
 // launches, or, where there is little to do, one after the other in one
-// workgroup (a launch costs 2.6 us, a barrier nothing).
+// workgroup (a launch costs 2.6 us, a barrier nothing).  Chains of latencies bound
+// them, not bytes: a phase is three to six loads or atomics that wait for one another
+// (0.5 - 1 us each), and its instructions, which no cache holds yet.  On the GPU,
+// us, by phase: fork to 3 children, 25 pages, 6.3; to 448, 15867 pages, 5.0 and 10.2;
+// grow of 6 rows, 203 pages, 9.2, of 384 rows, 92670 pages, 5.8 and 7.3; free of 2
+// rows 2.2, of 128 rows 3.6; compact of 76 pages 4.4, of 15485 pages, half of them
+// in use, 5.1, 7.0 and 4.0.  Copies of that many are at the memory's rate: 64 MB read
+// and written in 21.4 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
