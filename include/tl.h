@@ -696,6 +696,11 @@ int tl_kv_grow(const tl_kv_pages* pages, const int32_t* rows, const int32_t* len
  * rows[i] from the ceil(lens[i] / page_tokens)-th on (lens NULL: all of them)
  * become -1, and their pages lose a reference each.  Errors: as tl_kv_grow.
  * n == 0 enqueues nothing.
+ * A row that is cut inside a page which another row shares goes on sharing it,
+ * and tl_kv_grow leaves it alone: what tl_kv_append or tl_kv_keep then writes
+ * there overwrites the other row's tokens.  Where pages may be shared (after
+ * tl_kv_fork), a row that loses tokens is forked onto itself (tl_kv_fork), instead
+ * of this call or after it, before it is written on.
  */
 int tl_kv_free(const tl_kv_pages* pages, const int32_t* rows, const int32_t* lens, int32_t n, void* stream);
 
@@ -713,7 +718,11 @@ int tl_kv_free(const tl_kv_pages* pages, const int32_t* rows, const int32_t* len
  * src, dst, tokens: device int32 [n], the pairs in the order of the children:
  *             the parent's page, the child's, and the tokens in it; then -1.
  * count:      device int32 [2]: the pairs, and the children for which no page
- *             was free (their entry stays -1).  Always written.
+ *             was free (their entry is -1).  Always written.
+ * A row may be its own parent: it is cut to its first lens[i] tokens, and the
+ * page that they fill in part becomes its own as a child's does.  One that no
+ * other entry names stays as it is, without a pair; one for which no page is free
+ * stays, too, shared as before and counted, and the call may be repeated.
  * A row must not be a child twice, nor a child of one and the parent of another:
  * which tokens it ends up with is not specified then.
  * Errors: as tl_kv_grow.

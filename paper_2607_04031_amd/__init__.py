@@ -745,7 +745,8 @@ def kv_grow(pages: KVPages, rows, lens, missing=None, stream=None):
 
 
 def kv_free(pages: KVPages, rows, lens=None, stream=None):
-    """Rows of the table (int32 [n]) give their pages back, but for those of their first lens[i] tokens."""
+    """Rows of the table (int32 [n]) give their pages back, but for those of their first lens[i] tokens.  A row that is cut inside
+    a page that it shares is forked onto itself (kv_fork) before it is written on."""
     rc = (_calls or _load_calls()).kv_free(pages.desc, rows, lens, stream)
     if rc is not None:
         return _check(rc, "tl_kv_free")
@@ -758,7 +759,8 @@ def kv_free(pages: KVPages, rows, lens=None, stream=None):
 def kv_fork(pages: KVPages, parents, children, lens, out=None, stream=None):
     """Row children[i] of the table goes on from the first lens[i] tokens of row parents[i].  Returns (src, dst, tokens, count),
     the pairs of pages that kv_copy copies in every cache of the pool: int32 [n] three times, and [2]: the pairs, and the
-    children for which no page was free."""
+    children for which no page was free.  A row that is its own parent is cut to its first lens[i] tokens, and no other row
+    sees what is written to it then."""
     src, dst, tokens, count = out if out is not None else (None,) * 4
     rc = (_calls or _load_calls()).kv_fork(pages.desc, parents, children, lens, src, dst, tokens, count, stream)
     if rc is not None:

@@ -195,13 +195,14 @@ __device__ void grow_give(const PagesLaunch& a, const Crew& w, int32_t* pages) {
     }
 }
 
-// fork, first phase: which children need a page of their own
+// fork, first phase: which children need a page of their own; of the rows that are
+// their own parents those whose page another entry names too
 __device__ void fork_count(const PagesLaunch& a, const Crew& w) {
     for (int64_t i = w.wave * 64 + w.lane; i < a.n; i += w.waves * 64) {
-        const int32_t* from = row_of(a, a.parents[i]);
+        const int32_t *from = row_of(a, a.parents[i]), *to = row_of(a, a.rows[i]);
         const int64_t len = min(int64_t(max(a.lens[i], 0)), a.max_pages << a.log2_page), full = len >> a.log2_page;
-        const bool part = from && row_of(a, a.rows[i]) && (len & ((1 << a.log2_page) - 1));
-        a.want[i] = part && is_page(a, from[full]) ? 1 : 0;
+        const int page = from && to && (len & ((1 << a.log2_page) - 1)) ? from[full] : -1;
+        a.want[i] = is_page(a, page) && (from != to || a.refs[page] != 1) ? 1 : 0;
     }
 }
 // second phase: the children's rows, and the pairs to copy
@@ -212,13 +213,15 @@ __device__ void fork_give(const PagesLaunch& a, const Crew& w, int32_t* pages) {
         int32_t* to = a.n ? row_of(a, a.rows[i]) : nullptr;
         const int64_t len = from ? min(int64_t(max(a.lens[i], 0)), a.max_pages << a.log2_page) : 0;
         const int full = int(len >> a.log2_page), part = int(len & ((1 << a.log2_page) - 1));
+        const bool same = from && from == to;
+        const int kept = full + (same && part && !want);    // entries that go on as they are
         // the parent's entries are on their way while the child's own page is found
         int page[8], old = want ? from[full] : -1;
         auto load = [&](int64_t base) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int64_t at = base + 64 * j + w.lane;
-                page[j] = at < full ? from[at] : -1;
+                page[j] = at < kept ? from[at] : -1;
             }
         };
         load(0);
@@ -233,14 +236,16 @@ __device__ void fork_give(const PagesLaunch& a, const Crew& w, int32_t* pages) {
         int own = -1;
         if (want) {
             PageCursor c{0, 0};
-            if (page_take(a, w, rank, 1, &c, pages)) own = pages[0];
+            const bool found = page_take(a, w, rank, 1, &c, pages);
+            if (found) own = pages[0];
+            else if (same && is_page(a, old)) own = old;    // shared as before: nothing of the row is lost
             wave_sync();
-            if (own >= 0 && w.lane == 0) {
+            if (found && w.lane == 0) {
                 a.src[rank] = old;
                 a.dst[rank] = own;
                 a.tokens[rank] = part;
-                atomicAdd(&a.refs[own], 1);
             }
+            if (own >= 0 && w.lane == 0) atomicAdd(&a.refs[own], 1);
         }
         for (int64_t base = 0; base < a.max_pages; base += 64 * 8) {
             if (base) load(base);
@@ -248,7 +253,7 @@ __device__ void fork_give(const PagesLaunch& a, const Crew& w, int32_t* pages) {
             for (int j = 0; j < 8; ++j) {
                 const int64_t at = base + 64 * j + w.lane;
                 if (at >= a.max_pages) break;
-                const bool shared = at < full && is_page(a, page[j]);
+                const bool shared = at < kept && is_page(a, page[j]);
                 if (shared) atomicAdd(&a.refs[page[j]], 1);
                 page[j] = atomicExch(&to[at], shared ? page[j] : at == full ? own : -1);
             }
