@@ -683,7 +683,9 @@ typedef struct tl_kv_pages {
  * missing:    device int32 [1]: how many entries found no free page (they, and
  *             only they, stay negative), at most 2^31 - 1.  Always written.
  * A row that is named twice gets its pages once, which ones is not specified,
- * and 'missing' counts it twice.
+ * and 'missing' counts it twice.  What a page holds is left from whoever had it
+ * last: an entry that tokens were meant for already (of a child for which
+ * tl_kv_fork found no page) is not told from one of tokens to come.
  * Errors: TL_EINVAL for NULL or misaligned pointers (4 bytes), sizes below 1, a
  * bad page_tokens, more than 2^31 - 1 tokens, n < 0, or arrays that overlap;
  * TL_EUNSUPPORTED for max_pages above 2^25, num_rows * max_pages above 2^40 or n
@@ -719,6 +721,13 @@ int tl_kv_free(const tl_kv_pages* pages, const int32_t* rows, const int32_t* len
  *             the parent's page, the child's, and the tokens in it; then -1.
  * count:      device int32 [2]: the pairs, and the children for which no page
  *             was free (their entry is -1).  Always written.
+ * Pages go out in the children's order, so that the children without one are the
+ * last count[1] of those that need one.  They have their full pages alone, and the
+ * entry looks like one of tokens to come: a tl_kv_grow to lens[i] or more would give
+ * it a page that holds none of the parent's tokens, and count it as found.  So
+ * count[1] has to be known before such a row grows or is attended over beyond its
+ * full pages; once there are free pages (tl_kv_free), a fork of these children
+ * again, from the same parents, makes them whole.
  * A row may be its own parent: it is cut to its first lens[i] tokens, and the
  * page that they fill in part becomes its own as a child's does.  One that no
  * other entry names stays as it is, without a pair; one for which no page is free

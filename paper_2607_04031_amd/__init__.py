@@ -759,8 +759,8 @@ def kv_free(pages: KVPages, rows, lens=None, stream=None):
 def kv_fork(pages: KVPages, parents, children, lens, out=None, stream=None):
     """Row children[i] of the table goes on from the first lens[i] tokens of row parents[i].  Returns (src, dst, tokens, count),
     the pairs of pages that kv_copy copies in every cache of the pool: int32 [n] three times, and [2]: the pairs, and the
-    children for which no page was free.  A row that is its own parent is cut to its first lens[i] tokens, and no other row
-    sees what is written to it then."""
+    children for which no page was free: the last of those that need one, to be forked again, with pages free, before they
+    grow.  A row that is its own parent is cut to its first lens[i] tokens, and no other row sees what is written to it then."""
     src, dst, tokens, count = out if out is not None else (None,) * 4
     rc = (_calls or _load_calls()).kv_fork(pages.desc, parents, children, lens, src, dst, tokens, count, stream)
     if rc is not None:

@@ -1,5 +1,5 @@
 """Rows of a pool that share pages and are written again: a row that is its own parent in tl_kv_fork gets the last page that it
-fills in part for itself, and loses nothing where none is free."""
+fills in part for itself, and loses nothing where none is free; and forks that find too few pages, which are repeated."""
 import numpy as np
 import pytest
 
@@ -186,3 +186,29 @@ def test_nothing_is_lost_where_no_page_is_free():
     assert run.fork([0], [0], [70]) == [0, 0]
     run.write(0, 60)
     run.check()
+
+
+@pytest.mark.parametrize("elem", [2, tl.TL_KV_E2M1])
+def test_forks_that_find_too_few_pages_are_repeated(elem):
+    """The last of the children that need a page are those without one; forked again once pages are free, and only then given
+    pages for more tokens, they are what they would have been."""
+    banner(f"pages: forks without free pages, elem={elem}")
+    run = Run(elem, 6, 6)
+    run.write(0, 100)                                      # pages 0, 1
+    run.write(5, 130)                                      # pages 2, 3, 4
+    children, lens = [1, 2, 3, 4], [100, 64, 90, 100]      # the second needs no page of its own
+    assert run.fork([0] * 4, children, lens) == [1, 2]
+    needs = [c for c, n in zip(children, lens) if n % 64]
+    short = needs[len(needs) - 2:]
+    assert short == [3, 4] and (_get(run.pool.table)[short, 1] == -1).all() and (_get(run.pool.table)[short, 0] >= 0).all()
+    for r in short:
+        del run.text[r]
+    run.check()
+    tl.kv_free(run.pool, _int([5]))
+    del run.text[5]
+    assert run.fork([0, 0], short, [90, 100]) == [2, 0]
+    run.check()
+    for r in (0, 3, 4):
+        run.write(r, 20)
+    run.check()
+    assert int((run.pool.refs == 0).sum()) == 1            # of six pages one: rows 0, 1, 3 and 4 have a second page each
