@@ -35,11 +35,11 @@ __device__ inline void wait_for_lds_loads() {
 // result: of the first tile in its slot 2 w, of the last in 2 w + 1.
 constexpr int kTileCost = 96;
 struct Seq {
-    int seq, first, n, len;     // first: row of the first new token; n: new tokens; len: keys
-    int rows;                   // new tokens that are computed: those within the caller's bound
-    int tiles;                  // of rows
-    int cost, rise;             // places of tile t: cost + (t + 1) rise
-    int64_t before;             // places before the sequence
+    int seq = 0, first = 0, n = 0, len = 0;     // first: row of the first new token; n: new tokens; len: keys
+    int rows = 0;               // new tokens that are computed: those within the caller's bound
+    int tiles = 0;              // of rows
+    int cost = 0, rise = 0;     // places of tile t: cost + (t + 1) rise
+    int64_t before = 0;         // places before the sequence (where the longest tiles come first: not looked for)
 };
 
 // the new token of a row: row / group
@@ -227,9 +227,9 @@ __device__ inline bool attn_begin(const AttnLaunch& a, AttnLine* line, AttnRun* 
 // The piece that begins at r->place: chunks [chunk0, chunk1) of a tile of a head.
 struct AttnPiece {
     Seq s;
-    int head, tile, chunk0, chunk1;
-    bool whole;
-    int64_t slot;       // of its partial result, if it is not the whole tile
+    int head = 0, tile = 0, chunk0 = 0, chunk1 = 0;
+    bool whole = false;
+    int64_t slot = 0;   // of its partial result, if it is not the whole tile
 };
 
 // The tile at place p where the longest ones come first: sequence (one a lane),
