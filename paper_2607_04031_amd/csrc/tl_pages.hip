@@ -15,7 +15,7 @@
 // workgroup (a launch costs 2.6 us, a barrier nothing).  Chains of latencies bound
 // them, not bytes: a phase is three to six loads or atomics that wait for one another
 // (0.5 - 1 us each), and its instructions, which no cache holds yet.  On the GPU,
-// us, by phase: fork to 3 children, 25 pages, 6.3; to 448, 15867 pages, 5.0 and 10.2;
+// us, by phase: fork to 3 children, 25 pages, 6.6; to 448, 15867 pages, 5.0 and 10.2;
 // grow of 6 rows, 203 pages, 9.2, of 384 rows, 92670 pages, 5.8 and 7.3; free of 2
 // rows 2.2, of 128 rows 3.6; compact of 76 pages 4.4, of 15485 pages, half of them
 // in use, 5.1, 7.0 and 4.0.  Copies of that many are at the memory's rate: 64 MB read
@@ -214,14 +214,13 @@ __device__ void fork_give(const PagesLaunch& a, const Crew& w, int32_t* pages) {
         const int64_t len = from ? min(int64_t(max(a.lens[i], 0)), a.max_pages << a.log2_page) : 0;
         const int full = int(len >> a.log2_page), part = int(len & ((1 << a.log2_page) - 1));
         const bool same = from && from == to;
-        const int kept = full + (same && part && !want);    // entries that go on as they are
         // the parent's entries are on their way while the child's own page is found
         int page[8], old = want ? from[full] : -1;
         auto load = [&](int64_t base) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int64_t at = base + 64 * j + w.lane;
-                page[j] = at < kept ? from[at] : -1;
+                page[j] = at < full + (same && part) ? from[at] : -1;
             }
         };
         load(0);
@@ -233,6 +232,7 @@ __device__ void fork_give(const PagesLaunch& a, const Crew& w, int32_t* pages) {
             for (int64_t j = pairs + w.lane; j < a.n; j += 64) a.src[j] = a.dst[j] = a.tokens[j] = -1;
         }
         if (!to) continue;
+        const int kept = full + (same && part && !want);    // entries that go on as they are
         int own = -1;
         if (want) {
             PageCursor c{0, 0};
