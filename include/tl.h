@@ -711,7 +711,8 @@ int tl_kv_free(const tl_kv_pages* pages, const int32_t* rows, const int32_t* len
  * first lens[i] tokens of row parents[i] become those of row children[i].  Full
  * pages are shared (a reference more); a page that they fill in part is the
  * child's own, a free one, and a pair of pages to copy (tl_kv_copy, once for
- * every cache of the pool).  What the child's row held before loses its
+ * every cache of the pool, before anything else is written to them: a page that is
+ * copied may be free already).  What the child's row held before loses its
  * references; its other entries become -1.  A parent outside the table has no
  * tokens.
  *
