@@ -30,7 +30,7 @@
 // TB/s (6.3 in the middle; a workgroup's start takes over 3 us), and 4.7.  Few chunks per
 // workgroup are bound by its start and end: three chains of five tokens over
 // 131072, 8 heads over one, 30 us (2.5 TB/s) and 7 us, 4 bits 25 (conversions, made
-// by both waves that share the keys) and 7.6; one token over 517, 7 us, 4 bits 7.6.
+// by both waves that share the keys) and 7.6; one token over 517, 6.7 us, 4 bits 7.5.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>

@@ -7,14 +7,15 @@
 // instruction are 1 KB without gaps in LDS, so reads have no bank conflicts.
 //
 // Bound by the matrix and vector work of its waves, which hide one another's
-// only in part (MFMA busy for 36 % of the cycles, 8 bits 32 %, at 2.12 - 2.15
-// GHz), and by the starts and ends of pieces of tiles.  Three prompts, 135
+// only in part (MFMA busy for 36 % of the cycles, 8 bits 32 %, 4 bits 38 %, at 2.12 -
+// 2.15 GHz), and by the starts and ends of pieces of tiles.  Three prompts, 135
 // GFLOP, bf16: 153 - 155 us, the join of partial results 13.5; trees of 64
 // tokens, 107 GFLOP over 8-bit entries, 151 - 160 us, the join 10.3.  Prompts over
-// 4-bit entries, 135 GFLOP, 146 - 154 us without a join (whole tiles, the longest
-// first), 172 and 13.4 in equal parts: of a chunk's 3.7 thousand cycles a wave
-// converts for 674, loads for 378, multiplies for 937 and 1131, takes 405 for the softmax
-// and 199 at the barrier.  4 bits sum the weights, rounded as the products take
+// 4-bit entries, 135 GFLOP, 144 - 158 us without a join (whole tiles, the longest
+// first), 172 and 13.4 in equal parts: of a chunk's 3.7 thousand cycles (clock reads
+// in a copy of the kernel, which cost some themselves) a wave converts for 674,
+// loads for 378, multiplies for 937 and 1131, takes 405 for the softmax and 199 at
+// the barrier.  4 bits sum the weights, rounded as the products take
 // them, by a product with ones (2 of 34 MFMA, for 32 additions a lane), and have
 // both row tiles' softmax run side by side.
 #include <hip/hip_runtime.h>

@@ -15,11 +15,17 @@
 // workgroup (a launch costs 2.6 us, a barrier nothing).  Chains of latencies bound
 // them, not bytes: a phase is three to six loads or atomics that wait for one another
 // (0.5 - 1 us each), and its instructions, which no cache holds yet.  On the GPU,
-// us, by phase: fork to 3 children, 25 pages, 6.6; to 448, 15867 pages, 5.0 and 10.2;
+// us, by phase: fork to 3 children, 25 pages, 6.5; to 448, 15867 pages, 5.0 and 10.2;
 // grow of 6 rows, 203 pages, 9.2, of 384 rows, 92670 pages, 5.8 and 7.3; free of 2
 // rows 2.2, of 128 rows 3.6; compact of 76 pages 4.4, of 15485 pages, half of them
 // in use, 5.1, 7.0 and 4.0.  Copies of that many are at the memory's rate: 64 MB read
-// and written in 21.4 us.
+// and written in 21.6 us; 4-bit pages have half the bytes of 8-bit ones (8000 of 64
+// tokens of a head 19.6 us, 8 bits 34.2; 448 3.8 and 4.3).
+// Every row of grow and fork sums what the rows before it want, so that many rows
+// take the square of their number: grow and fork of 4096 rows 22 and 21 us, of
+// 16384 79 and 112, of 65536 667 and 1149.  A row's pages are found by one wave, 64 at a
+// time: those of a prompt of 8192 tokens (128) 15 us, of 32 such 26, of 131072 tokens
+// (2048) 194.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
